@@ -223,14 +223,14 @@ def _keep(s):
         k["desc"] = tb.make_linear_desc(rows, K, N, c["x"], c["y"], c["act"])
         k["ws"] = tb.alloc_linear_workspace(k["desc"])
         if c["pack"]:
-            k["x"] = tb.alloc_mx8(rows, K)
+            k["x"] = tb.alloc_mx(rows, K)
         width = N
     else:
         k["desc"] = tb.make_ffn_desc(rows, K, N, EPS, c["x"], c["w"], c["act"])
         k["ws"] = tb.alloc_ffn_workspace(k["desc"])
         width = K
     if c["op"] != "ffn" and c["y"] == "mx8":
-        k["q"] = tb.alloc_mx8(rows, width)
+        k["q"] = tb.alloc_mx(rows, width)
         k["y"] = torch.empty(rows, width, dtype=torch.bfloat16, device="cuda")
     else:
         k["y"] = torch.empty(rows, width, dtype=dt, device="cuda")
@@ -249,13 +249,13 @@ def _own(s):
     elif c["op"] == "linear":
         x, xs = s["x"], get("xs")
         if c["pack"]:
-            tb.toma_mx8_quantize(x, *k["x"])
+            tb.toma_mx_quantize(x, *k["x"])
             x, xs = k["x"]
         tb.toma_linear(desc, x, xs, s["w0"], get("ws0"), get("b0"), get("r"), y, ys, k["ws"])
     else:
         tb.toma_ffn(desc, s["x"], get("r"), get("g"), s["w0"], get("ws0"), get("b0"), s["w1"], get("ws1"), get("b1"), y, k["ws"])
     if ys is not None:
-        tb.toma_mx8_dequantize(y, ys, k["y"])
+        tb.toma_mx_dequantize(y, ys, k["y"])
     return {"h": k["h"], "y": k["y"]} if c["op"] == "norm" and c["res"] else {"y": k["y"]}
 
 
