@@ -9,7 +9,8 @@ A case is a dict:
     K, N    widths: input and output of a linear layer; a norm's width is K; a block's width is K and its hidden width N
     x       type of the input: "f32", "bf16", or "mx8" (8-bit elements with a power-of-two scale per 32 channels).  A linear layer
             with `pack` gets its input in bf16 and packs it in the call, as after an attention
-    y       type of the output: as x, or "mx8" behind a norm or an 8-bit product that another 8-bit product follows
+    y       type of the output: as x, "mx8" behind a norm that an 8-bit product follows, "bf16" behind an 8-bit product (inside
+            a block of 8-bit products the first one's output is "mx8" too)
     w       "ffn": type of the weights ("mx8": the whole block runs its products in 8 bits)
     act     "none", "gelu" (by erf), "gelu_tanh", "silu"
     bias, res   whether there is a bias (or a gain), a residual input
@@ -48,8 +49,8 @@ def listed():
         _case("linear_up_large", "linear", 16384, 4096, 8192, act="gelu"),
         # projection behind the attention of SDXL's second stage with text tokens, packed in the call
         _case("mx8_proj", "linear", 2 * (512 + 77), 1280, 1280, x="mx8", y="bf16", res=True, pack=True),
-        # the same large layer in 8 bits, its output for the next 8-bit product
-        _case("mx8_up_large", "linear", 16384, 4096, 8192, x="mx8", act="gelu"),
+        # the same large layer in 8 bits
+        _case("mx8_up_large", "linear", 16384, 4096, 8192, x="mx8", y="bf16", act="gelu"),
         # the feed-forward block of SDXL's second stage on merged tokens
         _case("ffn_sdxl2", "ffn", 1024, 1280, 5120, act="gelu", res=True),
         # the same of the first stage of a 128 x 128 grid, products in 8 bits
@@ -71,9 +72,8 @@ def draw(rng):
         elif op == "linear":
             x = rng.choice(["f32", "bf16", "bf16", "mx8", "mx8"])
             if x == "mx8":
-                y = rng.choice(["bf16", "mx8"])
-                c = _case("", op, log_int(1, 16384), 32 * log_int(2, 256), 32 * log_int(2, 256), x, y, act=act, bias=bias,
-                          res=res and y == "bf16", pack=rng.random() < 0.4)
+                c = _case("", op, log_int(1, 16384), 32 * log_int(2, 256), 8 * log_int(8, 1024), x, "bf16", act=act, bias=bias,
+                          res=res, pack=rng.random() < 0.4)
             else:
                 c = _case("", op, log_int(1, 16384), 8 * log_int(8, 1024), 8 * log_int(8, 1024), x, act=act, bias=bias, res=res)
         else:
@@ -202,7 +202,7 @@ def _plain(s):
         v = _act(_product(x, s, 0, mx8), c["act"])
         if "r" in s:
             v = v + s["r"].float()
-        return {"y": _value(*_pack(v)).to(torch.bfloat16) if c["y"] == "mx8" else v.to(dt)}
+        return {"y": v.to(dt)}
     h, n = _norm(s)
     u = _act(_product(_value(*_pack(n)) if mx8 else n, s, 0, mx8), c["act"])
     return {"y": (h + _product(_value(*_pack(u)) if mx8 else u, s, 1, mx8)).to(dt)}
@@ -218,6 +218,8 @@ def _keep(s):
     if c["op"] == "norm":
         k["desc"] = tb.make_norm_desc(rows, K, EPS, c["x"], c["y"])
         k["h"] = torch.empty(rows, K, dtype=dt, device="cuda") if c["res"] else None
+        if c["y"] == "mx8":
+            k["q"] = tb.alloc_mx(rows, K)
         width = K
     elif c["op"] == "linear":
         k["desc"] = tb.make_linear_desc(rows, K, N, c["x"], c["y"], c["act"])
@@ -229,11 +231,7 @@ def _keep(s):
         k["desc"] = tb.make_ffn_desc(rows, K, N, EPS, c["x"], c["w"], c["act"])
         k["ws"] = tb.alloc_ffn_workspace(k["desc"])
         width = K
-    if c["op"] != "ffn" and c["y"] == "mx8":
-        k["q"] = tb.alloc_mx(rows, width)
-        k["y"] = torch.empty(rows, width, dtype=torch.bfloat16, device="cuda")
-    else:
-        k["y"] = torch.empty(rows, width, dtype=dt, device="cuda")
+    k["y"] = torch.empty(rows, width, dtype=torch.bfloat16 if c["y"] == "mx8" else dt, device="cuda")
     return k
 
 
@@ -243,19 +241,19 @@ def _own(s):
     k, c = s["keep"], s["case"]
     tb, desc = k["tb"], k["desc"]
     get = s.get
-    y, ys = k["q"] if "q" in k else (k["y"], None)
     if c["op"] == "norm":
+        y, ys = k.get("q", (k["y"], None))
         tb.toma_rmsnorm(desc, s["x"], get("r"), get("g"), k["h"], y, ys)
+        if ys is not None:
+            tb.toma_mx_dequantize(y, ys, k["y"])
     elif c["op"] == "linear":
         x, xs = s["x"], get("xs")
         if c["pack"]:
             tb.toma_mx_quantize(x, *k["x"])
             x, xs = k["x"]
-        tb.toma_linear(desc, x, xs, s["w0"], get("ws0"), get("b0"), get("r"), y, ys, k["ws"])
+        tb.toma_linear(desc, x, xs, s["w0"], get("ws0"), get("b0"), get("r"), k["y"], None, k["ws"])
     else:
-        tb.toma_ffn(desc, s["x"], get("r"), get("g"), s["w0"], get("ws0"), get("b0"), s["w1"], get("ws1"), get("b1"), y, k["ws"])
-    if ys is not None:
-        tb.toma_mx_dequantize(y, ys, k["y"])
+        tb.toma_ffn(desc, s["x"], get("r"), get("g"), s["w0"], get("ws0"), get("b0"), s["w1"], get("ws1"), get("b1"), k["y"], k["ws"])
     return {"h": k["h"], "y": k["y"]} if c["op"] == "norm" and c["res"] else {"y": k["y"]}
 
 
@@ -297,8 +295,7 @@ def exact(case, seed):
 
     if case["op"] == "linear":
         x = d("x") if not mx8 else _grid(d("x")) if case["pack"] else _value(s["x"], s["xs"], torch.float64)
-        y = act(x @ weight(0) + d("b0")) + d("r")
-        return {"y": _grid(y) if case["y"] == "mx8" else y}
+        return {"y": act(x @ weight(0) + d("b0")) + d("r")}
     h = d("x") + d("r")
     n = h / torch.sqrt((h ** 2).sum(-1, keepdim=True) / case["K"] + EPS) * (d("g") if "g" in s else 1.0)
     if case["op"] == "norm":
