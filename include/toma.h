@@ -52,7 +52,9 @@ typedef enum {
   TOMA_ERR_LAUNCH = 6       /* the HIP runtime refused a launch */
 } toma_status;
 
-typedef enum { TOMA_F32 = 0, TOMA_BF16 = 1 } toma_dtype;
+/* TOMA_MX8 (operands of toma_linear, output of toma_rmsnorm; see toma_mx_quantize): 8-bit elements with a
+ * power-of-two scale per 32 consecutive channels. */
+typedef enum { TOMA_F32 = 0, TOMA_BF16 = 1, TOMA_MX8 = 2 } toma_dtype;
 
 /* Shape of one layer call (inputs of Alg. 3: X in R^{B x N x d}, D, tau). */
 typedef struct {
@@ -274,6 +276,97 @@ int toma_layer(const toma_desc *desc, const toma_attn_desc *attn, uint32_t reuse
  */
 int toma_mlp(int32_t dtype, int32_t rows, int32_t C, int32_t hidden, const void *In, const void *W1,
              const void *W2, void *Hbuf, void *Out, void *stream);
+
+/*
+ * The operators around the core modules of a block: the norm in front of a module, the linear layers, and the
+ * feed-forward block made of them, in bf16 or fp32 or with 8-bit products.  They take token rows (merged
+ * tokens, extra tokens, context, single conditioning vectors) and know nothing of regions.
+ *
+ * 8-bit tensors (TOMA_MX8) are two arrays: elements Q [rows, K], one e4m3 byte each, and scale codes
+ * S [rows, toma_mx_scale_stride(K)], one byte per 32 consecutive channels of a row; channel k of a row stands for
+ * Q * 2^(S[k / 32] - 127).  K % 32 == 0; bytes of S behind K / 32 are written as 0 and not interpreted.  Packing takes
+ * the smallest power of two by which the largest finite magnitude of the 32 fits 448 (2^-127 at least) and
+ * rounds the quotients to the nearest e4m3, ties to even; infinities and NaN become NaN.
+ *   toma_mx_quantize         X [rows, K] (x_type TOMA_F32 / TOMA_BF16) -> Q, S
+ *   toma_mx_quantize_weight  W [K, N] (w_type) -> Q [N, K], S [N, stride]: the layout in which a product takes its
+ *                            weights, blocks of 32 input channels of one output channel; once per weight
+ *   toma_mx_dequantize       Q, S -> Y [rows, K] in y_type: the values they stand for (bf16 holds all of them exactly, but
+ *                            for magnitudes below 2^-126)
+ * Limits: K <= 2^20, rows * max(K, 128) < 2^34; weights: K * N < 2^31.
+ */
+size_t toma_mx_scale_stride(int32_t K); /* 4 ceil(K / 128); 0 when K is not a positive multiple of 32 */
+int toma_mx_quantize(int32_t x_type, int32_t rows, int32_t K, const void *X, void *Q, void *S, void *stream);
+int toma_mx_quantize_weight(int32_t w_type, int32_t K, int32_t N, const void *W, void *Q, void *S, void *stream);
+int toma_mx_dequantize(int32_t y_type, int32_t rows, int32_t K, const void *Q, const void *S, void *Y, void *stream);
+
+/*
+ * Root-mean-square norm with the residual's addition, per row of C channels:
+ *   h = x + r;   y = h / sqrt(mean(h^2) + eps) * gamma
+ * The sum and the norm are evaluated in fp32 from the unrounded h.
+ *   X        in   [rows, C]       x_type
+ *   R_opt    in   [rows, C]       x_type; NULL: h = x
+ *   gamma_opt in  [C]             x_type; NULL: 1
+ *   H_opt    out  [rows, C]       h in x_type; may be X or R_opt itself; NULL: not wanted
+ *   Y        out  [rows, C]       y_type; with TOMA_MX8 the elements, and Ys_opt the scale codes; overlaps no input
+ * Limits: C % 32 == 0, C <= 16384, rows * max(C, 64) < 2^34; x_type TOMA_F32 / TOMA_BF16; y_type x_type or TOMA_MX8 (Ys_opt is non-NULL exactly then).
+ * Rows may be heads: the norm of 64-wide queries and keys is a call with C = 64 and rows = tokens * heads.
+ */
+typedef struct {
+  int32_t rows, C;
+  float eps;      /* > 0 */
+  int32_t x_type; /* toma_dtype of X, R, gamma, H */
+  int32_t y_type; /* toma_dtype of Y */
+} toma_norm_desc;
+int toma_rmsnorm(const toma_norm_desc *desc, const void *X, const void *R_opt, const void *gamma_opt, void *H_opt,
+                 void *Y, void *Ys_opt, void *stream);
+
+/*
+ * Linear layer with its epilogue: y = act(x W + bias) + r, from one row (a conditioning vector) to any number.
+ *   X         in   [rows, K]   x_type (TOMA_MX8: elements, Xs_opt their scale codes)
+ *   W         in   [K, N]      x_type, row-major, y = x W; with TOMA_MX8 instead elements [N, K] and Ws_opt their
+ *                              scale codes, as toma_mx_quantize_weight writes them
+ *   bias_opt  in   [N]         fp32 products: fp32; else bf16
+ *   R_opt     in   [rows, N]   as bias; may be Y itself
+ *   Y         out  [rows, N]   y_type (TOMA_MX8: elements, Ys_opt their scale codes); overlaps no other input
+ * Products accumulate in fp32, the epilogue is evaluated in fp32 and rounded once.
+ * Types: x_type TOMA_F32 / TOMA_BF16 with y_type the same; x_type TOMA_MX8 with y_type TOMA_BF16 or TOMA_MX8.
+ * Limits: TOMA_F32: K % 4 == 0, N % 4 == 0; TOMA_BF16: K % 8 == 0, N % 8 == 0; TOMA_MX8: K % 32 == 0 and N % 8 == 0 (y_type
+ * TOMA_MX8: N % 32 == 0).  K, N <= 2^20, rows <= 2^28, rows * max(K, N) < 2^34, K * N < 2^31.
+ * The scale-code arguments are non-NULL exactly where their tensor is TOMA_MX8.
+ */
+enum { TOMA_ACT_NONE = 0, TOMA_ACT_GELU = 1 /* x/2 (1 + erf(x / sqrt 2)) */, TOMA_ACT_GELU_TANH = 2, TOMA_ACT_SILU = 3 };
+typedef struct {
+  int32_t rows, K, N;
+  int32_t x_type, y_type; /* toma_dtype */
+  int32_t act;            /* TOMA_ACT_* */
+} toma_linear_desc;
+/* Bytes of scratch of toma_linear: 0 when the shape needs none (ws may then be NULL) or the descriptor is invalid. */
+size_t toma_linear_workspace_bytes(const toma_linear_desc *desc);
+int toma_linear(const toma_linear_desc *desc, const void *X, const void *Xs_opt, const void *W, const void *Ws_opt,
+                const void *bias_opt, const void *R_opt, void *Y, void *Ys_opt, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Feed-forward block on the residual stream, the two operators above in sequence:
+ *   h = x + r;   y = h + act(rmsnorm(h) W1 + b1) W2 + b2
+ * With w_type TOMA_MX8 both products run in 8 bits: the norm and the first product's epilogue write their outputs packed.
+ *   X, R_opt, Y   [rows, C]     x_type (TOMA_F32 / TOMA_BF16); Y may be X or R_opt itself
+ *   gamma_opt     [C];  b1_opt [hidden];  b2_opt [C]     x_type
+ *   W1 [C, hidden], W2 [hidden, C]  in x_type; w_type TOMA_MX8 (x_type TOMA_BF16 only): [hidden, C] and [C, hidden] packed
+ *                 by toma_mx_quantize_weight, with their scale codes
+ *   h and everything between lies in ws (toma_ffn_workspace_bytes, 256-byte aligned)
+ * Between the stages the norm's output, the hidden values and h are rounded to x_type (w_type TOMA_MX8: the first two packed).
+ * Limits: C % 32 == 0, C <= 16384, hidden % 32 == 0; sizes as for toma_linear.
+ */
+typedef struct {
+  int32_t rows, C, hidden;
+  float eps;
+  int32_t x_type, w_type; /* toma_dtype; w_type is x_type or TOMA_MX8 */
+  int32_t act;
+} toma_ffn_desc;
+size_t toma_ffn_workspace_bytes(const toma_ffn_desc *desc);
+int toma_ffn(const toma_ffn_desc *desc, const void *X, const void *R_opt, const void *gamma_opt, const void *W1,
+             const void *W1s_opt, const void *b1_opt, const void *W2, const void *W2s_opt, const void *b2_opt, void *Y,
+             void *ws, size_t ws_bytes, void *stream);
 
 /*
  * Profiling aid for benchmarks (not part of the method; for callers that want per-kernel times).

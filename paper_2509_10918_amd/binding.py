@@ -13,11 +13,14 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 # (a process started with TOMA_SANITIZE=1 loads the host-sanitizer build instead: CPU argument checks only)
 LIB_PATH = os.path.join(_HERE, "libtoma_san.so" if os.environ.get("TOMA_SANITIZE", "0") == "1" else "libtoma.so")
 
-TOMA_F32, TOMA_BF16 = 0, 1
+TOMA_F32, TOMA_BF16, TOMA_MX8 = 0, 1, 2
+ACTIVATIONS = {"none": 0, "gelu": 1, "gelu_tanh": 2, "silu": 3}
 TOMA_REUSE_IDX, TOMA_REUSE_A, TOMA_RECOMPUTE_WEIGHTS = 1, 2, 4
 EXPORTS = ("toma_workspace_bytes", "toma_status_string", "toma_select", "toma_select_static", "toma_merge", "toma_map_bytes",
            "toma_map_build", "toma_merge_cached", "toma_attend", "toma_cross_attend", "toma_unmerge", "toma_unmerge_pinv", "toma_recompute_cache_bytes", "toma_merge_recompute",
-           "toma_unmerge_recompute", "toma_layer", "toma_mlp", "toma_profile_enable",
+           "toma_unmerge_recompute", "toma_layer", "toma_mlp", "toma_mx_scale_stride", "toma_mx_quantize", "toma_mx_quantize_weight",
+           "toma_mx_dequantize", "toma_rmsnorm", "toma_linear_workspace_bytes", "toma_linear", "toma_ffn_workspace_bytes", "toma_ffn",
+           "toma_profile_enable",
            "toma_profile_kernel_name", "toma_profile_read", "toma_profile_map_product", "toma_profile_greedy_parts")
 
 
@@ -48,6 +51,21 @@ class toma_desc(ctypes.Structure):
 
 class toma_attn_desc(ctypes.Structure):
     _fields_ = [("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("t_extra", ctypes.c_int32)]
+
+
+class toma_norm_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("C", ctypes.c_int32), ("eps", ctypes.c_float), ("x_type", ctypes.c_int32),
+                ("y_type", ctypes.c_int32)]
+
+
+class toma_linear_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("K", ctypes.c_int32), ("N", ctypes.c_int32), ("x_type", ctypes.c_int32),
+                ("y_type", ctypes.c_int32), ("act", ctypes.c_int32)]
+
+
+class toma_ffn_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("C", ctypes.c_int32), ("hidden", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("x_type", ctypes.c_int32), ("w_type", ctypes.c_int32), ("act", ctypes.c_int32)]
 
 
 _lib = None
@@ -88,6 +106,17 @@ def lib():
         L.toma_unmerge_pinv.restype = ctypes.c_int
         L.toma_layer.argtypes = [vp, vp, ctypes.c_uint32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.toma_mlp.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, vp, vp, vp, vp, vp, vp]
+        i32 = ctypes.c_int32
+        L.toma_mx_scale_stride.restype = sz
+        L.toma_mx_scale_stride.argtypes = [i32]
+        L.toma_mx_quantize.argtypes = L.toma_mx_quantize_weight.argtypes = L.toma_mx_dequantize.argtypes = [i32, i32, i32, vp, vp, vp, vp]
+        L.toma_rmsnorm.argtypes = [vp] * 8
+        L.toma_linear_workspace_bytes.restype = L.toma_ffn_workspace_bytes.restype = sz
+        L.toma_linear_workspace_bytes.argtypes = L.toma_ffn_workspace_bytes.argtypes = [vp]
+        L.toma_linear.argtypes = [vp] * 10 + [sz, vp]
+        L.toma_ffn.argtypes = [vp] * 12 + [sz, vp]
+        for name in ("toma_mx_quantize", "toma_mx_quantize_weight", "toma_mx_dequantize", "toma_rmsnorm", "toma_linear", "toma_ffn"):
+            getattr(L, name).restype = ctypes.c_int
         for name in ("toma_select", "toma_merge", "toma_map_build", "toma_merge_cached", "toma_attend", "toma_cross_attend", "toma_unmerge", "toma_unmerge_pinv", "toma_recompute_cache_bytes", "toma_merge_recompute",
            "toma_unmerge_recompute",
                      "toma_layer", "toma_mlp"):
@@ -225,6 +254,135 @@ def toma_mlp(In, W1, W2, Hbuf, Out):
     code = TOMA_BF16 if In.dtype == torch.bfloat16 else TOMA_F32
     _check(lib().toma_mlp(code, rows, C, hidden, _ptr(In), _ptr(W1), _ptr(W2), _ptr(Hbuf), _ptr(Out), _stream()),
            "toma_mlp")
+
+
+# ---- operators around the core modules --------------------------------------------------------------
+# These check shapes, types and the device as well: the C ABI takes bare pointers.
+
+_TYPE = {torch.float32: TOMA_F32, torch.bfloat16: TOMA_BF16, "f32": TOMA_F32, "bf16": TOMA_BF16, "mx8": TOMA_MX8, TOMA_F32: TOMA_F32,
+         TOMA_BF16: TOMA_BF16, TOMA_MX8: TOMA_MX8}
+_TORCH = {TOMA_F32: torch.float32, TOMA_BF16: torch.bfloat16, TOMA_MX8: torch.uint8}
+
+
+def _arg(what, t, code, count):
+    """Pointer of a tensor argument after its checks; count: elements it has to hold."""
+    if t is None:
+        return None
+    if t.dtype != _TORCH[code] or t.numel() != count:
+        raise ValueError(f"{what}: {count} elements of {_TORCH[code]} expected, got {t.numel()} of {t.dtype}")
+    if not (t.is_cuda and t.is_contiguous()):
+        raise ValueError(f"{what}: libtoma takes contiguous CUDA tensors")
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{what} lies on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return t.data_ptr()
+
+
+def _scratch(ws):
+    """Pointer and bytes of a scratch tensor (None: no scratch)."""
+    return (None, 0) if ws is None else (_arg("ws", ws, TOMA_MX8, ws.numel()), ws.numel())
+
+
+def _scale_stride(K):
+    return 4 * ((K + 127) // 128)
+
+
+def toma_mx_scale_stride(K):
+    return lib().toma_mx_scale_stride(K)
+
+
+def alloc_mx(rows, K, device="cuda"):
+    """Elements and scale codes of an 8-bit tensor."""
+    stride = toma_mx_scale_stride(K)
+    if stride == 0:
+        raise TomaError(5, "toma_mx_scale_stride")
+    return (torch.empty((rows, K), dtype=torch.uint8, device=device),
+            torch.empty((rows, stride), dtype=torch.uint8, device=device))
+
+
+def toma_mx_quantize(X, Q, S):
+    """X [..., K] -> Q [rows, K], S [rows, stride] (alloc_mx)."""
+    rows, K = Q.shape
+    code = _TYPE.get(X.dtype, -1)
+    _check(lib().toma_mx_quantize(code, rows, K, _arg("X", X, max(code, 0), rows * K), _arg("Q", Q, TOMA_MX8, rows * K),
+                                  _arg("S", S, TOMA_MX8, rows * _scale_stride(K)), _stream()), "toma_mx_quantize")
+
+
+def toma_mx_quantize_weight(W, Q, S):
+    """W [K, N] -> Q [N, K], S [N, stride] (alloc_mx(N, K))."""
+    K, N = W.shape
+    code = _TYPE.get(W.dtype, -1)
+    _check(lib().toma_mx_quantize_weight(code, K, N, _arg("W", W, max(code, 0), K * N), _arg("Q", Q, TOMA_MX8, K * N),
+                                         _arg("S", S, TOMA_MX8, N * _scale_stride(K)), _stream()), "toma_mx_quantize_weight")
+
+
+def toma_mx_dequantize(Q, S, Y):
+    """The values of Q [rows, K], S as Y [..., K] (float32 or bfloat16)."""
+    rows, K = Q.shape
+    code = _TYPE.get(Y.dtype, -1)
+    _check(lib().toma_mx_dequantize(code, rows, K, _arg("Q", Q, TOMA_MX8, rows * K), _arg("S", S, TOMA_MX8, rows * _scale_stride(K)),
+                                    _arg("Y", Y, max(code, 0), rows * K), _stream()), "toma_mx_dequantize")
+
+
+def make_norm_desc(rows, C, eps, x_type, y_type=None):
+    return toma_norm_desc(rows, C, eps, _TYPE[x_type], _TYPE[x_type if y_type is None else y_type])
+
+
+def toma_rmsnorm(desc, X, R, gamma, H, Y, Ys=None):
+    n, x = desc.rows * desc.C, desc.x_type
+    _check(lib().toma_rmsnorm(_ref(desc), _arg("X", X, x, n), _arg("R", R, x, n), _arg("gamma", gamma, x, desc.C), _arg("H", H, x, n),
+                              _arg("Y", Y, desc.y_type, n), _arg("Ys", Ys, TOMA_MX8, desc.rows * _scale_stride(desc.C)), _stream()),
+           "toma_rmsnorm")
+
+
+def make_linear_desc(rows, K, N, x_type, y_type=None, act="none"):
+    return toma_linear_desc(rows, K, N, _TYPE[x_type], _TYPE[x_type if y_type is None else y_type], ACTIVATIONS[act])
+
+
+def toma_linear_workspace_bytes(desc):
+    return lib().toma_linear_workspace_bytes(_ref(desc))
+
+
+def _alloc_scratch(n, device):
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def alloc_linear_workspace(desc, device="cuda"):
+    """Scratch of toma_linear; None when the shape needs none."""
+    return _alloc_scratch(toma_linear_workspace_bytes(desc), device)
+
+
+def toma_linear(desc, X, Xs, W, Ws, bias, R, Y, Ys, ws):
+    rows, K, N, x = desc.rows, desc.K, desc.N, desc.x_type
+    e = TOMA_F32 if x == TOMA_F32 else TOMA_BF16   # bias and residual
+    p, n = _scratch(ws)
+    _check(lib().toma_linear(_ref(desc), _arg("X", X, x, rows * K), _arg("Xs", Xs, TOMA_MX8, rows * _scale_stride(K)), _arg("W", W, x, K * N),
+                             _arg("Ws", Ws, TOMA_MX8, N * _scale_stride(K)), _arg("bias", bias, e, N), _arg("R", R, e, rows * N),
+                             _arg("Y", Y, desc.y_type, rows * N), _arg("Ys", Ys, TOMA_MX8, rows * _scale_stride(N)), p, n, _stream()),
+           "toma_linear")
+
+
+def make_ffn_desc(rows, C, hidden, eps, x_type, w_type=None, act="gelu"):
+    return toma_ffn_desc(rows, C, hidden, eps, _TYPE[x_type], _TYPE[x_type if w_type is None else w_type], ACTIVATIONS[act])
+
+
+def toma_ffn_workspace_bytes(desc):
+    return lib().toma_ffn_workspace_bytes(_ref(desc))
+
+
+def alloc_ffn_workspace(desc, device="cuda"):
+    n = toma_ffn_workspace_bytes(desc)
+    if n == 0:
+        raise TomaError(5, "toma_ffn_workspace_bytes")
+    return _alloc_scratch(n, device)
+
+
+def toma_ffn(desc, X, R, gamma, W1, W1s, b1, W2, W2s, b2, Y, ws):
+    n, C, hidden, x, w = desc.rows * desc.C, desc.C, desc.hidden, desc.x_type, desc.w_type
+    p, nb = _scratch(ws)
+    _check(lib().toma_ffn(_ref(desc), _arg("X", X, x, n), _arg("R", R, x, n), _arg("gamma", gamma, x, C), _arg("W1", W1, w, C * hidden),
+                          _arg("W1s", W1s, TOMA_MX8, hidden * _scale_stride(C)), _arg("b1", b1, x, hidden), _arg("W2", W2, w, C * hidden),
+                          _arg("W2s", W2s, TOMA_MX8, C * _scale_stride(hidden)), _arg("b2", b2, x, C), _arg("Y", Y, x, n), p, nb, _stream()),
+           "toma_ffn")
 
 
 def toma_profile_enable(on):

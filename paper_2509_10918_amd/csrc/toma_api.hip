@@ -432,3 +432,156 @@ TOMA_API int toma_mlp(int32_t dtype, int32_t rows, int32_t C, int32_t hidden, co
     return TOMA_ERR_ALIGN;
   return launch_mlp(dtype, rows, C, hidden, In, W1, W2, Hbuf, Out, static_cast<hipStream_t>(stream));
 }
+
+// ---- operators around the core modules ----------------------------------------------------------
+
+static bool plain_type(int32_t t) { return t == TOMA_F32 || t == TOMA_BF16; }
+
+TOMA_API size_t toma_mx_scale_stride(int32_t K) { return K > 0 && K % 32 == 0 && K <= (1 << 20) ? (size_t)mx_scale_stride(K) : 0; }
+
+// Checks that the packing calls share; the plain tensor is P.
+static int check_pack(int32_t type, int32_t rows, int32_t K, const void *P, const void *Q, const void *S) {
+  if (!plain_type(type)) return TOMA_ERR_UNSUPPORTED;
+  if (rows <= 0 || K <= 0) return TOMA_ERR_SHAPE;
+  if (K % 32 || K > (1 << 20) || (long long)rows * std::max(K, 128) >= (1ll << 34)) return TOMA_ERR_UNSUPPORTED;
+  if (!P || !Q || !S) return TOMA_ERR_NULL;
+  if (misaligned(P, 16) || misaligned(Q, 16) || misaligned(S, 16)) return TOMA_ERR_ALIGN;
+  return TOMA_OK;
+}
+
+TOMA_API int toma_mx_quantize(int32_t x_type, int32_t rows, int32_t K, const void *X, void *Q, void *S, void *stream) {
+  const int rc = check_pack(x_type, rows, K, X, Q, S);
+  return rc != TOMA_OK ? rc : launch_mx_quantize(x_type, rows, K, X, Q, S, static_cast<hipStream_t>(stream));
+}
+
+TOMA_API int toma_mx_quantize_weight(int32_t w_type, int32_t K, int32_t N, const void *W, void *Q, void *S, void *stream) {
+  int rc = check_pack(w_type, N, K, W, Q, S);
+  if (rc == TOMA_OK && (N > (1 << 20) || (long long)K * N >= (1ll << 31))) rc = TOMA_ERR_UNSUPPORTED;
+  return rc != TOMA_OK ? rc : launch_mx_quantize_weight(w_type, K, N, W, Q, S, static_cast<hipStream_t>(stream));
+}
+
+TOMA_API int toma_mx_dequantize(int32_t y_type, int32_t rows, int32_t K, const void *Q, const void *S, void *Y, void *stream) {
+  const int rc = check_pack(y_type, rows, K, Y, Q, S);
+  return rc != TOMA_OK ? rc : launch_mx_dequantize(y_type, rows, K, Q, S, Y, static_cast<hipStream_t>(stream));
+}
+
+static int check_norm(const toma_norm_desc *d) {
+  if (!d) return TOMA_ERR_NULL;
+  if (d->rows <= 0 || d->C <= 0 || !(d->eps > 0.0f) || !isfinite(d->eps)) return TOMA_ERR_SHAPE;
+  if (!plain_type(d->x_type) || (d->y_type != d->x_type && d->y_type != TOMA_MX8)) return TOMA_ERR_UNSUPPORTED;
+  if (d->C % 32 || d->C > 16384 || (long long)d->rows * std::max(d->C, 64) >= (1ll << 34)) return TOMA_ERR_UNSUPPORTED;
+  return TOMA_OK;
+}
+
+TOMA_API int toma_rmsnorm(const toma_norm_desc *desc, const void *X, const void *R_opt, const void *gamma_opt, void *H_opt,
+                          void *Y, void *Ys_opt, void *stream) {
+  const int rc = check_norm(desc);
+  if (rc != TOMA_OK) return rc;
+  if (!X || !Y || (desc->y_type == TOMA_MX8) != (Ys_opt != nullptr)) return TOMA_ERR_NULL;
+  if (misaligned(X, 16) || misaligned(R_opt, 16) || misaligned(gamma_opt, 16) || misaligned(H_opt, 16) || misaligned(Y, 16) ||
+      misaligned(Ys_opt, 16))
+    return TOMA_ERR_ALIGN;
+  return launch_rmsnorm(*desc, X, R_opt, gamma_opt, H_opt, Y, Ys_opt, static_cast<hipStream_t>(stream));
+}
+
+static int check_linear(const toma_linear_desc *d) {
+  if (!d) return TOMA_ERR_NULL;
+  if (d->rows <= 0 || d->K <= 0 || d->N <= 0) return TOMA_ERR_SHAPE;
+  if (d->x_type == TOMA_MX8) {
+    if (d->y_type != TOMA_BF16 && d->y_type != TOMA_MX8) return TOMA_ERR_UNSUPPORTED;
+    if (d->K % 32 || d->N % (d->y_type == TOMA_MX8 ? 32 : 8)) return TOMA_ERR_UNSUPPORTED;
+  } else {
+    if (!plain_type(d->x_type) || d->y_type != d->x_type) return TOMA_ERR_UNSUPPORTED;
+    const int step = d->x_type == TOMA_BF16 ? 8 : 4;
+    if (d->K % step || d->N % step) return TOMA_ERR_UNSUPPORTED;
+  }
+  if (d->act < TOMA_ACT_NONE || d->act > TOMA_ACT_SILU) return TOMA_ERR_UNSUPPORTED;
+  if (d->K > (1 << 20) || d->N > (1 << 20) || d->rows > (1 << 28) || (long long)d->K * d->N >= (1ll << 31) ||
+      (long long)d->rows * std::max(d->K, d->N) >= (1ll << 34))
+    return TOMA_ERR_UNSUPPORTED;
+  return TOMA_OK;
+}
+
+TOMA_API size_t toma_linear_workspace_bytes(const toma_linear_desc *desc) {
+  return check_linear(desc) == TOMA_OK ? up256(linear_workspace_bytes(*desc)) : 0;
+}
+
+TOMA_API int toma_linear(const toma_linear_desc *desc, const void *X, const void *Xs_opt, const void *W, const void *Ws_opt,
+                         const void *bias_opt, const void *R_opt, void *Y, void *Ys_opt, void *ws, size_t ws_bytes,
+                         void *stream) {
+  const int rc = check_linear(desc);
+  if (rc != TOMA_OK) return rc;
+  const bool mx = desc->x_type == TOMA_MX8;
+  if (!X || !W || !Y || mx != (Xs_opt != nullptr) || mx != (Ws_opt != nullptr) ||
+      (desc->y_type == TOMA_MX8) != (Ys_opt != nullptr))
+    return TOMA_ERR_NULL;
+  if (misaligned(X, 16) || misaligned(Xs_opt, 16) || misaligned(W, 16) || misaligned(Ws_opt, 16) || misaligned(bias_opt, 16) ||
+      misaligned(R_opt, 16) || misaligned(Y, 16) || misaligned(Ys_opt, 16))
+    return TOMA_ERR_ALIGN;
+  const size_t need = linear_workspace_bytes(*desc);
+  if (need != 0) {
+    if (!ws) return TOMA_ERR_NULL;
+    if (misaligned(ws, 256)) return TOMA_ERR_ALIGN;
+    if (ws_bytes < need) return TOMA_ERR_WORKSPACE;
+  }
+  return launch_linear(*desc, X, Xs_opt, W, Ws_opt, bias_opt, R_opt, Y, Ys_opt, ws, static_cast<hipStream_t>(stream));
+}
+
+// The stages of a feed-forward block and where their outputs lie in the workspace.
+struct FfnPlan {
+  toma_norm_desc norm;
+  toma_linear_desc up, down;
+  size_t h, n, ns, u, us, lin, total;
+};
+static int plan_ffn(const toma_ffn_desc *d, FfnPlan *p) {
+  if (!d) return TOMA_ERR_NULL;
+  if (d->w_type != d->x_type && !(d->w_type == TOMA_MX8 && d->x_type == TOMA_BF16)) return TOMA_ERR_UNSUPPORTED;
+  p->norm = toma_norm_desc{d->rows, d->C, d->eps, d->x_type, d->w_type};
+  p->up = toma_linear_desc{d->rows, d->C, d->hidden, d->w_type, d->w_type, d->act};
+  p->down = toma_linear_desc{d->rows, d->hidden, d->C, d->w_type, d->x_type, TOMA_ACT_NONE};
+  int rc = check_norm(&p->norm);
+  if (rc == TOMA_OK) rc = check_linear(&p->up);
+  if (rc == TOMA_OK) rc = check_linear(&p->down);
+  if (rc != TOMA_OK) return rc;
+  if (d->hidden % 32) return TOMA_ERR_UNSUPPORTED;
+  const bool mx = d->w_type == TOMA_MX8;
+  const size_t rows = (size_t)d->rows, es = d->x_type == TOMA_F32 ? 4 : 2, ew = mx ? 1 : es;
+  size_t off = 0;
+  auto take = [&](size_t bytes) { const size_t o = off; off += up256(bytes); return o; };
+  p->h = take(rows * d->C * es);
+  p->n = take(rows * d->C * ew);
+  p->ns = take(mx ? rows * mx_scale_stride(d->C) : 0);
+  p->u = take(rows * d->hidden * ew);
+  p->us = take(mx ? rows * mx_scale_stride(d->hidden) : 0);
+  p->lin = take(std::max(linear_workspace_bytes(p->up), linear_workspace_bytes(p->down)));
+  p->total = off;
+  return TOMA_OK;
+}
+
+TOMA_API size_t toma_ffn_workspace_bytes(const toma_ffn_desc *desc) {
+  FfnPlan p;
+  return plan_ffn(desc, &p) == TOMA_OK ? p.total : 0;
+}
+
+TOMA_API int toma_ffn(const toma_ffn_desc *desc, const void *X, const void *R_opt, const void *gamma_opt, const void *W1,
+                      const void *W1s_opt, const void *b1_opt, const void *W2, const void *W2s_opt, const void *b2_opt, void *Y,
+                      void *ws, size_t ws_bytes, void *stream) {
+  FfnPlan p;
+  int rc = plan_ffn(desc, &p);
+  if (rc != TOMA_OK) return rc;
+  const bool mx = desc->w_type == TOMA_MX8;
+  if (!X || !W1 || !W2 || !Y || !ws || mx != (W1s_opt != nullptr) || mx != (W2s_opt != nullptr)) return TOMA_ERR_NULL;
+  if (misaligned(X, 16) || misaligned(R_opt, 16) || misaligned(gamma_opt, 16) || misaligned(W1, 16) || misaligned(W1s_opt, 16) ||
+      misaligned(b1_opt, 16) || misaligned(W2, 16) || misaligned(W2s_opt, 16) || misaligned(b2_opt, 16) || misaligned(Y, 16) ||
+      misaligned(ws, 256))
+    return TOMA_ERR_ALIGN;
+  if (ws_bytes < p.total) return TOMA_ERR_WORKSPACE;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  char *wsb = static_cast<char *>(ws);
+  void *h = R_opt ? static_cast<void *>(wsb + p.h) : nullptr, *ns = mx ? wsb + p.ns : nullptr, *us = mx ? wsb + p.us : nullptr;
+  rc = launch_rmsnorm(p.norm, X, R_opt, gamma_opt, h, wsb + p.n, ns, st);
+  if (rc != TOMA_OK) return rc;
+  rc = launch_linear(p.up, wsb + p.n, ns, W1, W1s_opt, b1_opt, nullptr, wsb + p.u, us, wsb + p.lin, st);
+  if (rc != TOMA_OK) return rc;
+  return launch_linear(p.down, wsb + p.u, us, W2, W2s_opt, b2_opt, h ? h : X, Y, nullptr, wsb + p.lin, st);
+}

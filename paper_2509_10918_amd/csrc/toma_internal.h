@@ -249,9 +249,21 @@ int launch_unmerge_pinv(const Shape &s, const void *A, const float *Z, const voi
 int launch_mlp(int dtype, int rows, int C, int hidden, const void *In, const void *W1, const void *W2, void *Hbuf,
                void *Out, hipStream_t st);
 
+// ---- operators around the core modules (toma_norm.hip, toma_linear.hip) ----
+inline int mx_scale_stride(int K) { return 4 * ((K + 127) / 128); }
+int launch_mx_quantize(int x_type, int rows, int K, const void *X, void *Q, void *S, hipStream_t st);
+int launch_mx_quantize_weight(int w_type, int K, int N, const void *W, void *Q, void *S, hipStream_t st);
+int launch_mx_dequantize(int y_type, int rows, int K, const void *Q, const void *S, void *Y, hipStream_t st);
+int launch_rmsnorm(const toma_norm_desc &d, const void *X, const void *R, const void *gamma, void *H, void *Y, void *Ys,
+                   hipStream_t st);
+size_t linear_workspace_bytes(const toma_linear_desc &d);
+int launch_linear(const toma_linear_desc &d, const void *X, const void *Xs, const void *W, const void *Ws, const void *bias,
+                  const void *R, void *Y, void *Ys, void *ws, hipStream_t st);
+
 // Kernel identifiers of the profiling aid (toma_profile_*): one per kernel of the path.
 enum KernelId { K_LIMBS = 0, K_GRAM, K_GREEDY, K_WSTATS, K_LSE, K_WWRITE, K_ZSUM, K_MERGE, K_QKV, K_ATTN, K_PROJ,
-                K_SCALE, K_UNMERGE, K_SPLIT, K_MLP_UP, K_MLP_DOWN, K_OCC, K_PINV_EIG, K_PINV_APPLY, K_MERGE_FUSED, K_UNMERGE_FUSED, K_WBOUNDS, K_LOCAL_MERGE, K_COUNT };
+                K_SCALE, K_UNMERGE, K_SPLIT, K_MLP_UP, K_MLP_DOWN, K_OCC, K_PINV_EIG, K_PINV_APPLY, K_MERGE_FUSED, K_UNMERGE_FUSED, K_WBOUNDS, K_LOCAL_MERGE,
+                K_NORM, K_MX_QUANTIZE, K_MX_DEQUANTIZE, K_LINEAR, K_COUNT };
 
 // Brackets one launch with HIP events on its stream while profiling is enabled; free otherwise.
 struct KernelTimer {

@@ -1,0 +1,478 @@
+"""The norm, linear, packing and feed-forward operators on the GPU against their plain forms in 64 bits.
+
+Tolerances.  A stored bf16 value is off by at most half a step, 2^-8 of the value; fp32 2^-24; e4m3 2^-4 of the value or, below the
+normal range, half of 2^-9 of the scale.  A product of K terms summed in fp32 in any order is off by at most K 2^-24 of the sum of
+the terms' magnitudes.  The 8-bit matrix instruction aligns its 128 products to the largest before it adds them: what it loses
+was measured at 2^-12.2 of the largest (a single instruction, random elements and scales); 2^-12 of the sum of the magnitudes is
+more than that.  The epilogue adds a few fp32 roundings (EPI).  The slopes of the activations are below 1.13."""
+import pytest
+import torch
+
+from paper_2509_10918_amd import binding as tb
+
+import operators_ref as ref
+
+pytestmark = pytest.mark.gpu
+HALF = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}
+EPI = 2.0 ** -20
+NAN = float("nan")
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def randn(g, *shape):
+    return torch.randn(*shape, generator=g, device="cuda")
+
+
+def within(got, want, tol):
+    d = (got.double() - want).abs() - tol
+    assert not torch.isnan(got.double()).any(), "NaN"
+    assert (d <= 0).all(), f"over the tolerance by {d.max().item():.3e} at {int(d.argmax())} of {d.numel()}: {got.reshape(-1)[d.argmax()].item()} {want.reshape(-1)[d.argmax()].item()}"
+
+
+# ---- packing ------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,K", [(1, 32), (3, 64), (5, 96), (2, 128), (7, 160), (33, 640), (129, 1280), (1000, 352)])
+def test_quantize_is_the_definition(dtype, rows, K):
+    print(f"[quantize] {dtype} {rows} x {K}", flush=True)
+    g = gen(rows * 1000 + K)
+    x = (randn(g, rows, K) * torch.exp2(torch.randint(-30, 30, (rows, K // 32, 1), generator=g, device="cuda").float()).expand(-1, -1, 32).reshape(rows, K)).to(DT[dtype])
+    x[0, :32] = 0
+    x.view(-1)[-1] = 448.0
+    xv, _ = ref.guarded(x, NAN)
+    q, s = tb.alloc_mx(rows, K)
+    qv, qc = ref.guarded(q.fill_(0x55), 0x33)
+    sv, sc = ref.guarded(s.fill_(0x55), 0x33)
+    tb.toma_mx_quantize(xv, qv, sv)
+    want = ref.pack(x)
+    assert torch.equal(sv, want[1]) and torch.equal(qv & 0x7f, want[0] & 0x7f)
+    assert torch.equal(ref.unpack(qv, sv), ref.unpack(*want))
+    qc(), sc()
+    for out in ("f32", "bf16"):
+        y, yc = ref.guarded(torch.empty(rows, K, dtype=DT[out]), 7.0)
+        tb.toma_mx_dequantize(qv, sv, y)
+        assert torch.equal(y.double(), ref.unpack(*want))
+        yc()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("K,N", [(32, 1), (64, 5), (96, 256), (160, 300), (640, 72), (1280, 1000)])
+def test_quantize_weight_is_quantize_of_the_transpose(dtype, K, N):
+    print(f"[quantize_weight] {dtype} {K} x {N}", flush=True)
+    w = randn(gen(K + N), K, N).to(DT[dtype])
+    wv, _ = ref.guarded(w, NAN)
+    q, s = tb.alloc_mx(N, K)
+    qv, qc = ref.guarded(q, 0x33)
+    sv, sc = ref.guarded(s.fill_(0x55), 0x33)
+    tb.toma_mx_quantize_weight(wv, qv, sv)
+    want = ref.pack(w.t().contiguous())
+    assert torch.equal(sv, want[1]) and torch.equal(ref.unpack(qv, sv), ref.unpack(*want))
+    qc(), sc()
+
+
+def test_quantize_of_extremes_and_values_that_are_not_finite():
+    for dt in (torch.float32, torch.bfloat16):
+        x = torch.zeros(8, 64, device="cuda")
+        x[0, 0], x[0, 1] = 449.0, -448.0
+        x[1, 3], x[1, 4] = float("inf"), -3.0
+        x[2, 3], x[2, 4] = NAN, 5.0
+        x[3, :] = float("-inf")
+        x[4, 0] = torch.finfo(torch.float32).max
+        x[5, 0], x[5, 40] = 2.0 ** -133, 2.0 ** -120
+        x[6, 31], x[6, 32] = 448.0 * 2.0 ** 20, 1.75 * 2.0 ** -10
+        x[7, 0] = 1e-38
+        x = x.to(dt)
+        q, s = tb.alloc_mx(8, 64)
+        tb.toma_mx_quantize(x, q, s)
+        want = ref.pack(x)
+        assert torch.equal(s, want[1])
+        a, b = ref.unpack(q, s), ref.unpack(*want)
+        assert torch.equal(torch.isnan(a), torch.isnan(b)) and torch.equal(torch.nan_to_num(a), torch.nan_to_num(b))
+
+
+# ---- norm ---------------------------------------------------------------------------------------------------------------
+
+def check_norm(x, r, g, eps, out, alias="", magnitude=1.0):
+    rows, C = x.shape
+    d = tb.make_norm_desc(rows, C, eps, x.dtype, out or x.dtype)
+    xv, xc = ref.guarded(x, NAN)
+    rv, rc = ref.guarded(r, NAN) if r is not None else (None, lambda: None)
+    gv, _ = ref.guarded(g, NAN) if g is not None else (None, None)
+    h, hc = ref.guarded(torch.full_like(x, 3.0), 7.0) if r is not None or alias == "none" else (None, lambda: None)
+    if alias == "x":
+        h, hc = xv, xc
+    elif alias == "r":
+        h, hc = rv, rc
+    h64, y64 = ref.norm(x, r, g, eps)
+    # the sum of squares: at most 64 additions in a row in a lane and eight over lanes and waves, then quotient, root, reciprocal and
+    # two products; the residual's addition rounds h once
+    rel = (64 + 8 + 8) * 2.0 ** -24
+    if out == "mx8":
+        q, s = tb.alloc_mx(rows, C)
+        qv, qc = ref.guarded(q.fill_(0x55), 0x33)
+        sv, sc = ref.guarded(s.fill_(0x55), 0x33)
+        tb.toma_rmsnorm(d, xv, rv, gv, h, qv, sv)
+        lo, hi = ref.codes(y64 * (1 - rel)), ref.codes(y64 * (1 + rel))
+        got = sv[:, :C // 32].long()
+        assert ((got >= lo) & (got <= hi)).all()
+        assert not sv[:, C // 32:].any()
+        scale = torch.exp2(got.double() - 127).repeat_interleave(32, 1)
+        within(ref.unpack(qv, sv), y64, y64.abs() * (2.0 ** -4 + 2 * rel) + scale * 2.0 ** -10)
+        qc(), sc()
+    else:
+        y, yc = ref.guarded(torch.empty_like(x), 7.0)
+        tb.toma_rmsnorm(d, xv, rv, gv, h, y)
+        within(y, y64, y64.abs() * (HALF[x.dtype] + 2 * rel) + 1e-30)
+        yc()
+    if h is not None:
+        within(h, h64, h64.abs() * HALF[x.dtype])
+        hc()
+    xc(), rc()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("out", ["", "mx8"])
+@pytest.mark.parametrize("rows,C,res,gain", [
+    (1, 32, False, False), (1, 64, True, True), (3, 96, True, False), (205, 64, True, True), (37, 128, False, True), (9, 160, True, True),
+    (5, 256, True, True), (130, 640, True, True), (33, 1024, False, True), (17, 1056, True, True), (65, 1280, True, True), (3, 4096, True, True), (2, 4128, True, False),
+    (5, 8192, True, True), (1, 16384, True, True), (2, 15904, False, False), (4099, 64, False, True)])
+def test_norm(dtype, out, rows, C, res, gain):
+    print(f"[norm] {dtype} -> {out or dtype} {rows} x {C} residual={res} gain={gain}", flush=True)
+    g = gen(rows + C)
+    x = (randn(g, rows, C) * torch.exp2(torch.randint(-6, 7, (rows, 1), generator=g, device="cuda").float())).to(DT[dtype])
+    r = randn(g, rows, C).to(DT[dtype]) if res else None
+    gamma = (1 + 0.3 * randn(g, C)).to(DT[dtype]) if gain else None
+    check_norm(x, r, gamma, 1e-6, out)
+
+
+@pytest.mark.parametrize("alias", ["x", "r", "none"])
+def test_norm_stores_the_sum_in_place(alias):
+    g = gen(5)
+    x, r = (randn(g, 70, 640).to(torch.bfloat16) for _ in range(2))
+    check_norm(x, r if alias != "none" else None, None, 1e-5, "", alias)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_norm_of_zero_tiny_and_huge_rows(dtype):
+    g = gen(6)
+    x = randn(g, 6, 96)
+    x[0] = 0
+    x[1] *= 1e-20
+    x[2] *= 1e15
+    x[3, 1:] = 0
+    x[4] *= 1e-3
+    check_norm(x.to(DT[dtype]), None, None, 1e-6, "")
+    check_norm(x.to(DT[dtype]), None, None, 1e-6, "mx8")
+
+
+# ---- linear ---------------------------------------------------------------------------------------------------------------
+
+def linear_case(x_type, y_type, rows, K, N, act, bias, res, seed=0, scale=1.0):
+    """Inputs on the GPU, the result in 64 bits and what it may be off."""
+    g = gen(seed + rows + 3 * K + 7 * N)
+    e = torch.float32 if x_type == "f32" else torch.bfloat16
+    x, w = randn(g, rows, K) * scale, randn(g, K, N) * K ** -0.5
+    b = randn(g, N).to(e) if bias else None
+    r = randn(g, rows, N).to(e) if res else None
+    if x_type == "mx8":
+        x, w = ref.pack(x.to(torch.bfloat16)), ref.pack(w.t().contiguous())
+        x64, w64 = ref.unpack(*x), ref.unpack(*w).t().contiguous()
+    else:
+        x, w = (x.to(e), None), (w.to(e), None)
+        x64, w64 = x[0].double(), w[0].double()
+    pre = x64 @ w64 + (b.double() if bias else 0.0)
+    size = x64.abs() @ w64.abs() + (b.double().abs() if bias else 0.0)
+    y = ref.act(pre, act) + (r.double() if res else 0.0)
+    tol = 1.13 * size * (K * 2.0 ** -24 + (2.0 ** -12 if x_type == "mx8" else 0.0)) + EPI * (pre.abs() + y.abs())
+    return x, w, b, r, y, tol
+
+
+def run_linear(x_type, y_type, x, w, b, r, act, in_place=False):
+    rows, K = x[0].shape
+    N = w[0].shape[0] if x_type == "mx8" else w[0].shape[1]
+    d = tb.make_linear_desc(rows, K, N, x_type, y_type, act)
+    ws = tb.alloc_linear_workspace(d)
+    if ws is not None:
+        ws, wc = ref.guarded(ws.fill_(0xff), 0x33)     # (NaN wherever fp32 is read unwritten)
+        assert ws.data_ptr() % 256 == 0
+    bad = 0x7f if x_type == "mx8" else NAN
+    xv = [ref.guarded(t, bad)[0] if t is not None else None for t in x]
+    wv = [ref.guarded(t, bad)[0] if t is not None else None for t in w]
+    bv = ref.guarded(b, NAN)[0] if b is not None else None
+    rv, rc = ref.guarded(r, NAN) if r is not None else (None, None)
+    checks = []
+    if y_type == "mx8":
+        q, s = tb.alloc_mx(rows, N)
+        (yv, yc), (sv, sc) = ref.guarded(q.fill_(0x55), 0x33), ref.guarded(s.fill_(0x55), 0x33)
+        checks = [yc, sc]
+    elif in_place:
+        yv, yc, sv = rv, rc, None
+        checks = [yc]
+    else:
+        e = torch.float32 if x_type == "f32" else torch.bfloat16
+        (yv, yc), sv = ref.guarded(torch.empty(rows, N, dtype=e), 7.0), None
+        checks = [yc]
+    tb.toma_linear(d, xv[0], xv[1], wv[0], wv[1], bv, rv, yv, sv, ws)
+    for c in checks + ([wc] if ws is not None else []):
+        c()
+    return yv, sv
+
+
+def check_linear(x_type, y_type, rows, K, N, act, bias, res, in_place=False, scale=1.0):
+    print(f"[linear] {x_type}->{y_type} {rows} x {K} x {N} {act} bias={bias} residual={res}", flush=True)
+    x, w, b, r, want, tol = linear_case(x_type, y_type, rows, K, N, act, bias, res, scale=scale)
+    y, s = run_linear(x_type, y_type, x, w, b, r, act, in_place)
+    if y_type == "mx8":
+        assert not s[:, N // 32:].any()
+        got = s[:, :N // 32].long()
+        assert ((got >= ref.codes(want.abs() - torch.minimum(tol, want.abs()))) & (got <= ref.codes(want.abs() + tol))).all()
+        sc = torch.exp2(got.double() - 127).repeat_interleave(32, 1)
+        within(ref.unpack(y, s), want, (want.abs() + tol) * 2.0 ** -4 + sc * 2.0 ** -10 + tol)
+    else:
+        within(y, want, (want.abs() + tol) * HALF[y.dtype] + tol)
+    return y
+
+
+SHAPES = [(1, 8, 8), (1, 64, 640), (2, 1280, 648), (3, 104, 72), (4, 2048, 128), (7, 640, 264), (8, 72, 1416), (15, 352, 136), (16, 4096, 64), (17, 64, 64),
+          (31, 96, 256), (32, 640, 640), (33, 1288, 24), (63, 128, 136), (64, 512, 264), (65, 200, 72), (100, 2560, 128), (128, 640, 256), (129, 64, 392),
+          (200, 1288, 520), (257, 96, 264), (300, 32, 1032), (511, 640, 384), (640, 192, 640), (1025, 320, 136)]
+
+
+@pytest.mark.parametrize("i", range(len(SHAPES)))
+@pytest.mark.parametrize("x_type", ["bf16", "f32"])
+def test_linear(x_type, i):
+    rows, K, N = SHAPES[i]
+    if x_type == "f32" and i % 3 == 1:
+        K, N = K + 4, N + 4          # fp32 needs multiples of four only
+    check_linear(x_type, x_type, rows, K, N, ref.ACTS[i % 4], i % 5 != 0, i % 2 == 0)
+
+
+MX_SHAPES = [(1, 32, 8), (1, 640, 640), (2, 1280, 648), (3, 96, 72), (4, 2048, 128), (7, 640, 264), (8, 160, 1416), (16, 4096, 64), (17, 64, 64), (31, 96, 256),
+             (33, 1312, 24), (63, 128, 136), (64, 512, 264), (65, 224, 72), (100, 2560, 128), (128, 640, 256), (129, 64, 392), (200, 1312, 520),
+             (257, 96, 264), (300, 32, 1032), (511, 640, 384), (640, 192, 640), (1025, 320, 136), (589, 1280, 1280)]
+
+
+@pytest.mark.parametrize("i", range(len(MX_SHAPES)))
+@pytest.mark.parametrize("y_type", ["bf16", "mx8"])
+def test_linear_mx(y_type, i):
+    rows, K, N = MX_SHAPES[i]
+    if y_type == "mx8":
+        N = (N + 31) // 32 * 32
+    check_linear("mx8", y_type, rows, K, N, ref.ACTS[i % 4], i % 5 != 0, i % 2 == 0)
+
+
+@pytest.mark.parametrize("x_type,rows,K,N", [("bf16", 2048, 1024, 2048), ("bf16", 2000, 1000, 1992), ("bf16", 4096, 640, 2560), ("bf16", 3000, 2560, 640),
+                                             ("mx8", 2048, 1024, 2048), ("mx8", 2000, 992, 1992), ("mx8", 4096, 640, 2560), ("mx8", 3000, 2560, 640),
+                                             ("f32", 1500, 640, 1000)])
+def test_linear_of_many_rows(x_type, rows, K, N):
+    y_type = "bf16" if x_type == "mx8" else x_type
+    check_linear(x_type, y_type, rows, K, N, "gelu", True, True)
+    if x_type == "mx8":
+        check_linear(x_type, "mx8", rows, K, (N + 31) // 32 * 32, "silu", True, False)
+
+
+@pytest.mark.parametrize("x_type", ["bf16", "f32", "mx8"])
+@pytest.mark.parametrize("rows", [1, 5, 48, 700])
+def test_linear_adds_to_the_residual_in_place(x_type, rows):
+    check_linear(x_type, "bf16" if x_type == "mx8" else x_type, rows, 640, 320, "none", True, True, in_place=True)
+
+
+@pytest.mark.parametrize("act", ref.ACTS)
+@pytest.mark.parametrize("x_type", ["bf16", "f32", "mx8"])
+def test_activations_over_their_range(x_type, act):
+    """Pre-activations from about -40 to 40, where exponentials leave the range and the tails cancel."""
+    check_linear(x_type, "bf16" if x_type == "mx8" else x_type, 96, 64, 512, act, True, False, scale=12.0)
+
+
+@pytest.mark.parametrize("x_type", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [1, 3, 40, 300])
+def test_linear_of_values_that_are_not_finite(x_type, rows):
+    """A row with an infinity or NaN gives what the formula gives, and no other row notices."""
+    K, N = 640, 136
+    x, w, b, r, want, tol = linear_case(x_type, x_type, rows, K, N, "none", True, False)
+    bad = rows // 2
+    x[0][bad, 3] = float("inf")
+    y, _ = run_linear(x_type, x_type, x, w, b, r, "none")
+    keep = [i for i in range(rows) if i != bad]
+    within(y[keep], want[keep], (want[keep].abs() + tol[keep]) * HALF[y.dtype] + tol[keep])
+    assert torch.equal(y[bad].double(), torch.where(w[0][3].double() > 0, 1.0, -1.0).to(torch.float64) * float("inf")) or (w[0][3] == 0).any()
+
+
+def test_linear_repeats_bit_for_bit():
+    for x_type, y_type, rows, K, N in (("bf16", "bf16", 3, 4096, 640), ("bf16", "bf16", 700, 2560, 640), ("f32", "f32", 100, 1024, 256), ("mx8", "bf16", 5, 4096, 640),
+                                       ("mx8", "mx8", 700, 2560, 640)):
+        x, w, b, r, _, _ = linear_case(x_type, y_type, rows, K, N, "gelu", True, True)
+        first = run_linear(x_type, y_type, x, w, b, r, "gelu")
+        for _ in range(3):
+            again = run_linear(x_type, y_type, x, w, b, r, "gelu")
+            assert all(p is None or torch.equal(p, q) for p, q in zip(first, again))
+
+
+# ---- feed-forward block -----------------------------------------------------------------------------------------------------
+
+def ffn_inputs(rows, C, hidden, x_type, w_type, res, bias, seed=0):
+    g = gen(seed + rows + C + hidden)
+    e = DT[x_type]
+    t = {"X": randn(g, rows, C).to(e), "R": randn(g, rows, C).to(e) if res else None, "gamma": (1 + 0.1 * randn(g, C)).to(e) if bias else None,
+         "b1": (0.1 * randn(g, hidden)).to(e) if bias else None, "b2": (0.1 * randn(g, C)).to(e) if bias else None}
+    w1, w2 = randn(g, C, hidden) * C ** -0.5, randn(g, hidden, C) * hidden ** -0.5
+    if w_type == "mx8":
+        t["W1"], t["W1s"] = tb.alloc_mx(hidden, C)
+        t["W2"], t["W2s"] = tb.alloc_mx(C, hidden)
+        tb.toma_mx_quantize_weight(w1.to(e), t["W1"], t["W1s"])
+        tb.toma_mx_quantize_weight(w2.to(e), t["W2"], t["W2s"])
+    else:
+        t["W1"], t["W2"], t["W1s"], t["W2s"] = w1.to(e), w2.to(e), None, None
+    return t
+
+
+def ffn_stages(t, d, act):
+    """The same block by the single operators."""
+    rows, C, hidden = d.rows, d.C, d.hidden
+    mx = d.w_type == tb.TOMA_MX8
+    e = t["X"].dtype
+    h = torch.empty_like(t["X"])
+    n, ns = tb.alloc_mx(rows, C) if mx else (torch.empty_like(h), None)
+    u, us = tb.alloc_mx(rows, hidden) if mx else (torch.empty(rows, hidden, dtype=e, device="cuda"), None)
+    y = torch.empty_like(h)
+    wt, w8 = ("mx8", "bf16") if mx else (e, e)
+    tb.toma_rmsnorm(tb.make_norm_desc(rows, C, d.eps, e, wt), t["X"], t["R"], t["gamma"], h, n, ns)
+    up, down = tb.make_linear_desc(rows, C, hidden, wt, wt, act), tb.make_linear_desc(rows, hidden, C, wt, w8)
+    tb.toma_linear(up, n, ns, t["W1"], t["W1s"], t["b1"], None, u, us, tb.alloc_linear_workspace(up))
+    tb.toma_linear(down, u, us, t["W2"], t["W2s"], t["b2"], h, y, None, tb.alloc_linear_workspace(down))
+    return y
+
+
+def ffn_call(t, d, y, ws):
+    tb.toma_ffn(d, t["X"], t["R"], t["gamma"], t["W1"], t["W1s"], t["b1"], t["W2"], t["W2s"], t["b2"], y, ws)
+
+
+@pytest.mark.parametrize("x_type,w_type", [("bf16", "bf16"), ("f32", "f32"), ("bf16", "mx8")])
+@pytest.mark.parametrize("rows,C,hidden,res,bias", [(1, 64, 256, True, True), (5, 320, 1280, False, True), (77, 96, 416, True, False), (333, 640, 2560, True, True),
+                                                    (1024, 352, 1408, False, False)])
+def test_ffn(x_type, w_type, rows, C, hidden, res, bias):
+    print(f"[ffn] {x_type}/{w_type} {rows} x {C} x {hidden}", flush=True)
+    t = ffn_inputs(rows, C, hidden, x_type, w_type, res, bias)
+    d = tb.make_ffn_desc(rows, C, hidden, 1e-6, x_type, w_type, "gelu")
+    ws, wc = ref.guarded(tb.alloc_ffn_workspace(d).fill_(0xff), 0x33)
+    y, yc = ref.guarded(torch.empty_like(t["X"]), 7.0)
+    ffn_call(t, d, y, ws)
+    yc(), wc()
+    assert torch.equal(y, ffn_stages(t, d, "gelu"))
+    # against 64 bits: the norm's output and the hidden values carry one rounding to the stage's type each (step / 2 = half), whose
+    # errors pass the products like their inputs do; they are independent, so the norm of the error is that of the roundings
+    h, n = ref.norm(t["X"], t["R"], t["gamma"], 1e-6)
+    w1, w2 = (ref.unpack(t[k], t[k + "s"]).t() if w_type == "mx8" else t[k].double() for k in ("W1", "W2"))
+    b1, b2 = (t[k].double() if t[k] is not None else 0.0 for k in ("b1", "b2"))
+    u = ref.act(n @ w1.contiguous() + b1, "gelu")
+    want = h + u @ w2.contiguous() + b2
+    half = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "mx8": 2.0 ** -4}[w_type]
+    # (an error of at most half relative to each element, met twice and once more in the output; slopes below 1.13, fp32 sums
+    # add far less for mx8 and bf16, and K 2^-24 of the terms' magnitudes, about sqrt(K) of the result, for fp32)
+    tol = 1.13 * half * ((want - h).norm() + u.norm() / u.numel() ** 0.5 * want.numel() ** 0.5) + HALF[DT[x_type]] * want.norm() * 2
+    tol = tol + (hidden + C) * 2.0 ** -24 * hidden ** 0.5 * (want - h).norm() * (x_type == "f32")
+    assert (y.double() - want).norm() <= tol, ((y.double() - want).norm().item(), tol.item())
+
+
+def test_ffn_updates_the_stream_in_place():
+    for x_type, w_type, res in (("bf16", "bf16", False), ("bf16", "mx8", True), ("f32", "f32", False)):
+        t = ffn_inputs(130, 320, 640, x_type, w_type, res, True)
+        d = tb.make_ffn_desc(130, 320, 640, 1e-6, x_type, w_type, "silu")
+        want = ffn_stages(t, d, "silu")
+        ws = tb.alloc_ffn_workspace(d)
+        y = t["R"] if res else t["X"]
+        ffn_call(t, d, y, ws)
+        assert torch.equal(y, want)
+
+
+@pytest.mark.parametrize("w_type", ["bf16", "mx8"])
+@pytest.mark.parametrize("rows", [2, 600])
+def test_ffn_replayed_from_a_graph(w_type, rows):
+    """Captured on a side stream, replayed on new inputs, between eager calls that share nothing with it."""
+    d = tb.make_ffn_desc(rows, 640, 2560, 1e-6, "bf16", w_type, "gelu")
+    t = ffn_inputs(rows, 640, 2560, "bf16", w_type, True, True)
+    ws, ws2 = tb.alloc_ffn_workspace(d), tb.alloc_ffn_workspace(d)
+    y, y2 = torch.empty_like(t["X"]), torch.empty_like(t["X"])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        ffn_call(t, d, y, ws)
+    for k in range(4):
+        new = ffn_inputs(rows, 640, 2560, "bf16", w_type, True, True, seed=100 + k)
+        for name in ("X", "R"):
+            t[name].copy_(new[name])
+        ffn_call(t, d, y2, ws2)
+        y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, y2), k
+
+
+def test_calls_on_two_streams_at_once():
+    """Two calls of each operator in flight on streams of their own, each with its own scratch."""
+    d = tb.make_ffn_desc(40, 640, 2560, 1e-6, "bf16", "mx8", "gelu")
+    ts = [ffn_inputs(40, 640, 2560, "bf16", "mx8", True, True, seed=s) for s in (1, 2)]
+    want = [ffn_stages(t, d, "gelu") for t in ts]
+    ws = [tb.alloc_ffn_workspace(d) for _ in ts]
+    ys = [torch.empty_like(t["X"]) for t in ts]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in ts]
+    for _ in range(5):
+        for k, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                ffn_call(ts[k], d, ys[k], ws[k])
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(ys, want))
+
+
+# ---- all of it in a block on merged tokens ------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("w_type", ["bf16", "mx8"])
+def test_pre_norm_block_on_merged_tokens(w_type):
+    """merge -> norm -> attention -> projection with residual -> feed-forward block -> unmerge, as a block that merges once
+    runs it; the stages between the merge and the unmerge against their plain forms on the same inputs."""
+    from paper_2509_10918_amd import synth
+    import toma_gpu as tg
+    w = synth.scaled(synth.WORKLOADS["sdxl1"], name="block", B=2, H=32, W=32, C=320, heads=5, index=61)
+    inp = synth.make_inputs(w)
+    dv = tg.Device(w, inp, 1)
+    dv.select()
+    dv.merge()
+    C, rows = w.C, w.B * w.D
+    g = gen(9)
+    gamma = (1 + 0.1 * randn(g, C)).to(torch.bfloat16)
+    wo, bo = (randn(g, C, C) * C ** -0.5).to(torch.bfloat16), (0.1 * randn(g, C)).to(torch.bfloat16)
+    h = dv.Xm.reshape(rows, C)
+    n = torch.empty_like(h)
+    tb.toma_rmsnorm(tb.make_norm_desc(rows, C, 1e-6, "bf16"), h, None, gamma, None, n)
+    within(n, ref.norm(h, None, gamma, 1e-6)[1], ref.norm(h, None, gamma, 1e-6)[1].abs() * (2.0 ** -8 + 1e-5) + 1e-30)
+    O = torch.empty_like(h)
+    tb.toma_attend(dv.desc, dv.attn, n, None, dv.Wq, dv.Wk, dv.Wv, None, O, dv.ws)
+    if w_type == "mx8":
+        wq, a = tb.alloc_mx(C, C), tb.alloc_mx(rows, C)
+        tb.toma_mx_quantize_weight(wo, *wq)
+        tb.toma_mx_quantize(O, *a)
+        d = tb.make_linear_desc(rows, C, C, "mx8", "bf16")
+        x64, w64 = ref.unpack(*a), ref.unpack(*wq).t().contiguous()
+    else:
+        wq, a = (wo, None), (O, None)
+        d = tb.make_linear_desc(rows, C, C, "bf16")
+        x64, w64 = O.double(), wo.double()
+    h2 = torch.empty_like(h)
+    tb.toma_linear(d, a[0], a[1], wq[0], wq[1], bo, h, h2, None, tb.alloc_linear_workspace(d))
+    want = x64 @ w64 + bo.double() + h.double()
+    within(h2, want, want.abs() * 2.0 ** -8 + (x64.abs() @ w64.abs() + 1) * 2.0 ** -11)
+    t = ffn_inputs(rows, C, 4 * C, "bf16", w_type, False, True)
+    t["X"] = h2
+    df = tb.make_ffn_desc(rows, C, 4 * C, 1e-6, "bf16", w_type, "gelu")
+    y = torch.empty_like(h)
+    ffn_call(t, df, y, tb.alloc_ffn_workspace(df))
+    assert torch.equal(y, ffn_stages(t, df, "gelu"))
+    dv.O.copy_(y.reshape(dv.O.shape))
+    Y = dv.unmerge()
+    assert torch.isfinite(torch.as_tensor(Y)).all()
