@@ -1,27 +1,9 @@
 // Linear layer with its epilogue: Y = act(X W + bias) + R.
-#include "toma_gemm.h"
-#include "toma_internal.h"
-#include "toma_mx.h"
+#include <stdlib.h>
+
+#include "toma_linear.h"
 
 namespace toma {
-
-// ---- epilogue, in fp32 ------------------------------------------------------------------------------------------------
-__device__ __forceinline__ float act_f32(float v, int act) {
-  if (act == TOMA_ACT_GELU) return 0.5f * v * (1.0f + erff(v * 0.70710678118654752f));
-  // x/2 (1 + tanh(u)) = x / (1 + exp(-2u)), u = sqrt(2/pi) (x + 0.044715 x^3)
-  if (act == TOMA_ACT_GELU_TANH) {
-    const float u = 0.79788456080286536f * v * __builtin_fmaf(0.044715f * v, v, 1.0f);
-    return v / (1.0f + __expf(-2.0f * u));
-  }
-  if (act == TOMA_ACT_SILU) return v / (1.0f + __expf(-v));
-  return v;
-}
-__device__ __forceinline__ f32x4 load4(const float *p) { return *reinterpret_cast<const f32x4 *>(p); }
-__device__ __forceinline__ f32x4 load4(const bf16_t *p) {
-  const u32x2 r = *reinterpret_cast<const u32x2 *>(p);
-  return (f32x4){__builtin_bit_cast(float, r[0] << 16), __builtin_bit_cast(float, r[0] & 0xffff0000u),
-                 __builtin_bit_cast(float, r[1] << 16), __builtin_bit_cast(float, r[1] & 0xffff0000u)};
-}
 
 template <typename T> struct EpiPol {
   static constexpr bool A_KS = false, B_KS = true, SPLIT_K = false, ACC_T = true;
@@ -50,8 +32,9 @@ template <typename T> struct EpiPol {
         const int m = m_w + 16 * i + c;
         if (m >= x.M) continue;
         f32x4 v = acc.t[i][j] + b;
-#pragma unroll
-        for (int r = 0; r < 4; r++) v[r] = act_f32(v[r], act);
+        float e[4] = {v[0], v[1], v[2], v[3]};
+        activate<sizeof(T) == 4>(e, act);
+        v = (f32x4){e[0], e[1], e[2], e[3]};
         const size_t at = (size_t)m * x.N + n;
         if (R) v += load4(R + at);
         store4<T>(Out + at, v);
@@ -63,6 +46,10 @@ template <typename T> struct EpiPol {
 template <typename T>
 static int linear_typed(const toma_linear_desc &d, const void *X, const void *W, const void *bias, const void *R, void *Y,
                         hipStream_t st) {
+  if (sizeof(T) == 2 && !getenv("LIN_OLD")) {
+    LinArgs a{X, W, nullptr, nullptr, bias, R, nullptr, Y, nullptr, d.rows, d.K, d.N, d.act, 0, 0};
+    return launch_linear_tile(0, a, false, st);
+  }
   EpiPol<T> p{};
   p.In = static_cast<const T *>(X); p.Wt = static_cast<const T *>(W); p.bias = static_cast<const T *>(bias);
   p.R = static_cast<const T *>(R); p.Out = static_cast<T *>(Y);
@@ -74,22 +61,13 @@ static int linear_typed(const toma_linear_desc &d, const void *X, const void *W,
 // ---- 8-bit products ---------------------------------------------------------------------------------------------------
 // v_mfma_scale_f32_16x16x128_f8f6f4: lane l holds row / column l % 16; its first 16 bytes are k = 16 g .. 16 g + 15 and its second
 // 64 + 16 g .. (g = l / 16), and the scale code it supplies is that of the block k = 32 g .. 32 g + 31.
-typedef int i32x8 __attribute__((ext_vector_type(8)));
 __device__ __forceinline__ f32x4 mma_mx(const i32x8 &a, const i32x8 &b, const f32x4 &c, uint32_t sa, uint32_t sb) {
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, (int)sa, 0, (int)sb);
 }
 
-struct MxArgs {
-  const uint8_t *X, *Xs, *W, *Ws;
-  const bf16_t *bias, *R;
-  void *Y;
-  uint8_t *Ys;
-  int rows, K, N, act, xs_stride, ys_stride;
-};
-
 // 32 x 32 outputs per wave, fragments straight from memory.
 template <bool MX_OUT>
-__global__ __launch_bounds__(256) void k_linear_mx(const MxArgs a) {
+__global__ __launch_bounds__(256) void k_linear_mx(const LinArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g = lane >> 4, c = lane & 15;
   const int tiles_n = (a.N + 63) / 64;
   const int m0 = (int)(blockIdx.x / tiles_n) * 64 + (w >> 1) * 32, n0 = (int)(blockIdx.x % tiles_n) * 64 + (w & 1) * 32;
@@ -98,8 +76,8 @@ __global__ __launch_bounds__(256) void k_linear_mx(const MxArgs a) {
 #pragma unroll
   for (int i = 0; i < 2; i++) {
     const int m = min(m0 + 16 * i + c, a.rows - 1), n = min(n0 + 16 * i + c, a.N - 1);
-    px[i] = a.X + (size_t)m * a.K; sx[i] = a.Xs + (size_t)m * a.xs_stride;
-    pw[i] = a.W + (size_t)n * a.K; sw[i] = a.Ws + (size_t)n * a.xs_stride;
+    px[i] = static_cast<const uint8_t *>(a.X) + (size_t)m * a.K; sx[i] = a.Xs + (size_t)m * a.xs_stride;
+    pw[i] = static_cast<const uint8_t *>(a.W) + (size_t)n * a.K; sw[i] = a.Ws + (size_t)n * a.xs_stride;
     acc[i][0] = acc[i][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
   }
   auto half = [&](const uint8_t *p, int k) { return k < a.K ? *reinterpret_cast<const u32x4 *>(p + k) : (u32x4){0u, 0u, 0u, 0u}; };
@@ -130,10 +108,11 @@ __global__ __launch_bounds__(256) void k_linear_mx(const MxArgs a) {
       const int n = n0 + 16 * j + 4 * g;
       const bool in = m < a.rows && n < a.N;
       v[j] = acc[i][j];
-      if (a.bias && in) v[j] += load4(a.bias + n);
-#pragma unroll
-      for (int r = 0; r < 4; r++) v[j][r] = act_f32(v[j][r], a.act);
-      if (a.R && in) v[j] += load4(a.R + (size_t)m * a.N + n);
+      if (a.bias && in) v[j] += load4(static_cast<const bf16_t *>(a.bias) + n);
+      float e[4] = {v[j][0], v[j][1], v[j][2], v[j][3]};
+      activate<false>(e, a.act);
+      v[j] = (f32x4){e[0], e[1], e[2], e[3]};
+      if (a.R && in) v[j] += load4(static_cast<const bf16_t *>(a.R) + (size_t)m * a.N + n);
       if (!MX_OUT && in) store4<bf16_t>(static_cast<bf16_t *>(a.Y) + (size_t)m * a.N + n, v[j]);
     }
     if constexpr (MX_OUT) {  // N % 32 == 0: the 32 columns of this wave are in or out together
@@ -161,9 +140,9 @@ __global__ __launch_bounds__(256) void k_linear_mx(const MxArgs a) {
 
 static int linear_mx(const toma_linear_desc &d, const void *X, const void *Xs, const void *W, const void *Ws, const void *bias,
                      const void *R, void *Y, void *Ys, hipStream_t st) {
-  MxArgs a{static_cast<const uint8_t *>(X), static_cast<const uint8_t *>(Xs), static_cast<const uint8_t *>(W), static_cast<const uint8_t *>(Ws),
-           static_cast<const bf16_t *>(bias), static_cast<const bf16_t *>(R), Y, static_cast<uint8_t *>(Ys),
-           d.rows, d.K, d.N, d.act, mx_scale_stride(d.K), mx_scale_stride(d.N)};
+  LinArgs a{X, W, static_cast<const uint8_t *>(Xs), static_cast<const uint8_t *>(Ws), bias, R, nullptr, Y, static_cast<uint8_t *>(Ys),
+            d.rows, d.K, d.N, d.act, mx_scale_stride(d.K), mx_scale_stride(d.N)};
+  if (!getenv("LIN_OLD")) return launch_linear_tile(1, a, Ys != nullptr, st);
   const dim3 grid((unsigned)(((d.rows + 63) / 64) * (long long)((d.N + 63) / 64)));
   KernelTimer kt(K_LINEAR, st);
   if (Ys) hipLaunchKernelGGL(k_linear_mx<true>, grid, dim3(256), 0, st, a);

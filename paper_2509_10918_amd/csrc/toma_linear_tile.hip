@@ -1,0 +1,371 @@
+// Tiled product of the linear layer for many rows: bf16, and 8 bits with a power-of-two scale per 32 channels.
+//
+// A workgroup computes BM x BN outputs, a wave WTM x WTN of them with the 16 x 16 matrix instructions (the 32 x 32 ones reach 1.79
+// instead of 2.10 PFLOP/s in bf16 on random data, 4.1 instead of 4.5 in 8 bits), the weights as first operand, so that a lane holds
+// one row and four consecutive columns of each.  K advances by 128 bytes of a row of X per step (128 channels in 8 bits, 64 in
+// bf16: whole cache lines), through two stages in LDS that the load-to-LDS path fills.
+// A 128-byte row of a stage is eight 16-byte packets; packet p of row r lies at place p ^ (r >> 1 & 7), which spreads the 16 rows
+// that a fragment read takes over all banks.
+#include <stdlib.h>
+
+#include "toma_linear.h"
+
+namespace toma {
+
+enum { LIN_BF16 = 0, LIN_MX = 1 };
+
+// One load-to-LDS instruction through a buffer descriptor: lane l's 16 bytes at base + off land at lds_addr + 16 l, zeros for a lane
+// whose offset is kNoPacket or beyond `bytes` (both uniform).
+constexpr uint32_t kNoPacket = 0x80000000u;  // (tiles span less than 2^30 bytes)
+__device__ __forceinline__ void buffer_to_lds16(const uint8_t *base, uint32_t bytes, uint32_t off, uint32_t lds_addr) {
+  const uint64_t b = (uint64_t)base;
+  const u32x4 rsrc = {(uint32_t)b, (uint32_t)(b >> 32), bytes, 0x00020000u};
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds_addr), "v"(off), "s"(rsrc) : "memory", "m0");
+}
+
+// place of packet pi of k-row k in a k-major stage of PPR packets a row: four rows of 32 bytes that a transpose read takes together
+// fall on the four quarters of 256 bytes, the rows eight further on (the upper half of the wave) on what they leave
+template <int PPR> __device__ __forceinline__ int km_place(int k, int pi) {
+  if constexpr (PPR >= 16) return pi ^ ((k & 3) << 2) ^ (((k >> 3) & 1) << 1);
+  return pi ^ (((k >> 1) & 1) << 2) ^ (((k >> 3) & 1) << 1);
+}
+
+template <int KIND, int BM, int BN, int WM, int WN, bool MX_OUT>
+__global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a, int tiles_m, int tiles_n) {
+  constexpr int NW = WM * WN, WTM = BM / WM, WTN = BN / WN, TM = WTM / 16, TN = WTN / 16;
+  constexpr int ES = KIND == LIN_MX ? 1 : 2, BK = 128 / ES;
+  constexpr int NIA = BM / 16 / NW, NIB = BN / 8 / NW;  // load instructions (1 KiB) per wave and step: half of X's rows, W
+  constexpr int NS = (BM + BN) / 64, NIS = KIND == LIN_MX ? (NS + NW - 1) / NW : 0;  // and the scale codes
+  constexpr int NLO = NIA + NIB + NIS, NHI = NIA;
+  constexpr int PPR = BN / 8;                          // packets per k-row of a k-major stage
+  static_assert(NIA >= 1 && NIB >= 1 && TM >= 4 && TM % 4 == 0 && TN <= 4, "every wave loads its share");
+  constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, S_BYTES = KIND == LIN_MX ? (BM + BN) * 4 : 0;
+  constexpr int B_AT = 2 * A_BYTES, S_AT = B_AT + 2 * B_BYTES, LDS_BYTES = S_AT + 2 * S_BYTES;
+  __shared__ __align__(1024) uint8_t lds[LDS_BYTES];
+
+  int tile_m, tile_n;
+  tile_of(blockIdx.x, gridDim.x, tiles_m, tiles_n, tile_m, tile_n);
+  const int m0 = tile_m * BM, n0 = tile_n * BN;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), wm = w / WN, wn = w % WN;
+  const int g = lane >> 4, c = lane & 15;
+  const int K = a.K, nk = (K + BK - 1) / BK;
+
+  // ---- loads: wave-uniform bases that advance with K, fixed byte offsets per lane -----------------------------------
+  const uint8_t *xb = static_cast<const uint8_t *>(a.X) + (size_t)m0 * K * ES;
+  const uint8_t *wb = static_cast<const uint8_t *>(a.W) + (KIND == LIN_MX ? (size_t)n0 * K : (size_t)n0 * 2);
+  const size_t w_step = KIND == LIN_MX ? 128 : (size_t)BK * a.N * 2;
+  // first row of the wave's t-th group of eight rows of X in the lower (upper) half of the row blocks of each wave row
+  auto x_row = [&](int t, bool upper) {
+    const int q = w * NIA + t;
+    return q / (WTM / 16) * WTM + q % (WTM / 16) * 8 + (upper ? WTM / 2 : 0);
+  };
+  // (rows and columns behind the end repeat the last: their results are not stored)
+  uint32_t xo[2][NIA], wo[NIB];
+#pragma unroll
+  for (int h = 0; h < 2; h++)
+#pragma unroll
+    for (int t = 0; t < NIA; t++) {
+      const int row = x_row(t, h) + (lane >> 3), p = (lane & 7) ^ ((row >> 1) & 7);
+      xo[h][t] = (uint32_t)min(row, a.rows - 1 - m0) * (uint32_t)(K * ES) + p * 16;
+    }
+#pragma unroll
+  for (int t = 0; t < NIB; t++) {
+    if constexpr (KIND == LIN_MX) {
+      const int row = (w * NIB + t) * 8 + (lane >> 3), p = (lane & 7) ^ ((row >> 1) & 7);
+      wo[t] = (uint32_t)min(row, a.N - 1 - n0) * (uint32_t)K + p * 16;
+    } else {
+      constexpr int RPI = 64 / PPR;  // k-rows per load instruction
+      const int k = (w * NIB + t) * RPI + lane / PPR, p = km_place<PPR>(k, lane % PPR);
+      wo[t] = (uint32_t)k * (uint32_t)(a.N * 2) + (uint32_t)min(p * 16, (a.N - n0 - 8) * 2);
+    }
+  }
+  // scale codes: a load instruction brings the four codes of 128 channels of 64 rows (of X, then of W)
+  const uint32_t l0 = lds_addr_of(lds);
+  const uint8_t *sb[NIS + 1];
+  uint32_t so[NIS + 1], ls[NIS + 1];
+#pragma unroll
+  for (int t = 0; t < NIS; t++) {
+    const int sr = (w * NIS + t) % NS * 64;
+    const bool of_x = sr < BM;
+    sb[t] = of_x ? a.Xs + (size_t)m0 * a.xs_stride : a.Ws + (size_t)n0 * a.xs_stride;
+    so[t] = (uint32_t)min(sr + lane - (of_x ? 0 : BM), of_x ? a.rows - 1 - m0 : a.N - 1 - n0) * (uint32_t)a.xs_stride;
+    ls[t] = l0 + S_AT + (uint32_t)sr * 4;
+  }
+
+  // Loads of step j into its stage in two parts: W, codes and the lower half of X's row blocks, and the upper half.  Packets behind
+  // the end of K, and all of a step behind the last, are zeros that nothing is read for.
+  auto issue_x = [&](uint32_t st, int j, auto upper_) {
+    constexpr int h = decltype(upper_)::value;
+    const uint32_t bytes = j < nk ? 0x40000000u : 0u;
+    const int left = K - j * BK;
+#pragma unroll
+    for (int t = 0; t < NIA; t++) {
+      const int k = ((lane & 7) ^ (((x_row(t, h) + (lane >> 3)) >> 1) & 7)) * (16 / ES);
+      buffer_to_lds16(xb + (size_t)j * 128, bytes, k < left ? xo[h][t] : kNoPacket, l0 + st * A_BYTES + (uint32_t)(x_row(t, h) * 128));
+    }
+  };
+  auto issue_lo = [&](uint32_t st, int j) {
+    if constexpr (KIND == LIN_MX) {
+#pragma unroll
+      for (int t = 0; t < NIS; t++)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(ls[t] + st * S_BYTES), "v"(so[t]),
+                     "s"(sb[t] + min(j, nk - 1) * 4)
+                     : "memory", "m0");
+    }
+    const uint32_t bytes = j < nk ? 0x40000000u : 0u;
+    const int left = K - j * BK;
+#pragma unroll
+    for (int t = 0; t < NIB; t++) {
+      const int k = KIND == LIN_MX ? ((lane & 7) ^ ((((w * NIB + t) * 8 + (lane >> 3)) >> 1) & 7)) * 16 : (w * NIB + t) * (64 / PPR) + lane / PPR;
+      buffer_to_lds16(wb + (size_t)j * w_step, bytes, k < left ? wo[t] : kNoPacket, l0 + B_AT + st * B_BYTES + (uint32_t)((w * NIB + t) * 1024));
+    }
+    issue_x(st, j, std::integral_constant<int, 0>());
+  };
+  auto meet = [&]() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+
+  // ---- fragments: a lane takes packets g and 4 + g of its row (bf16: one of each half of the step) ------------------------
+  // LDS addresses of the stage that is read; they move to the other stage at the end of a step
+  const uint32_t p0 = (uint32_t)(g ^ ((c >> 1) & 7)) << 4;
+  const int kq = 8 * g + (c >> 2), kcol = wn * WTN + 4 * (c & 3);  // (k-major weights: transpose reads)
+  constexpr int NRW = KIND == LIN_MX ? 2 : TN;
+  typedef __attribute__((address_space(3))) const uint8_t *lds_ptr;
+  lds_ptr rx[2], rw[NRW], rs = (lds_ptr)(lds + S_AT + c * 4);
+#pragma unroll
+  for (int e = 0; e < 2; e++) rx[e] = (lds_ptr)(lds + (wm * WTM + c) * 128 + (p0 ^ (64u * e)));
+#pragma unroll
+  for (int e = 0; e < NRW; e++) {
+    if constexpr (KIND == LIN_MX) rw[e] = (lds_ptr)(lds + B_AT + (wn * WTN + c) * 128 + (p0 ^ (64u * e)));
+    else rw[e] = (lds_ptr)(lds + B_AT + (kq * PPR + km_place<PPR>(kq, (kcol + 16 * e) >> 3)) * 16 + (kcol & 7) * 2);
+  }
+  typedef __attribute__((address_space(3))) const u32x4 *lds_u32x4_ptr;
+  typedef __attribute__((address_space(3))) const uint32_t *lds_u32_ptr;
+  typedef s16x4 __attribute__((address_space(3))) *lds_s16x4_ptr;
+  auto join = [](u32x4 a, u32x4 b) { return __builtin_bit_cast(i32x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7)); };
+  auto read_x = [&](int i) { return join(*(lds_u32x4_ptr)(rx[0] + i * 2048), *(lds_u32x4_ptr)(rx[1] + i * 2048)); };
+  auto read_w = [&](int j) {
+    if constexpr (KIND == LIN_MX) {
+      return join(*(lds_u32x4_ptr)(rw[0] + j * 2048), *(lds_u32x4_ptr)(rw[1] + j * 2048));
+    } else {
+      u32x4 f[2];
+#pragma unroll
+      for (int e = 0; e < 2; e++) {
+        const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(rw[j] + 32 * e * PPR * 16)));
+        const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(rw[j] + (32 * e + 4) * PPR * 16)));
+        f[e] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3);
+      }
+      return join(f[0], f[1]);
+    }
+  };
+  // scale codes of a step: byte b of word q is the code of row block 4 q + b for this lane's block of 32 channels (g)
+  constexpr int QX = (TM + 3) / 4, QW = (TN + 3) / 4;
+  uint32_t cx[QX], cw[QW], raw_x[TM], raw_w[TN];
+  auto read_codes = [&]() {
+#pragma unroll
+    for (int i = 0; i < TM; i++) raw_x[i] = *(lds_u32_ptr)(rs + (wm * WTM + 16 * i) * 4);
+#pragma unroll
+    for (int j = 0; j < TN; j++) raw_w[j] = *(lds_u32_ptr)(rs + (BM + wn * WTN + 16 * j) * 4);
+  };
+  const uint32_t tail_mask = K % 128 ? 0xffffffffu >> (32 - (K >> 5) % 4 * 8) : 0u;  // codes of the last group that stand for channels
+  auto gather = [&](const uint32_t *d, int n, uint32_t mask) {
+    const uint32_t sel = (uint32_t)g | (uint32_t)(4 + g) << 8;  // byte g of the second, then of the first operand
+    const uint32_t lo = __builtin_amdgcn_perm(n > 1 ? d[1] & mask : 0u, d[0] & mask, sel);
+    const uint32_t hi = n > 2 ? __builtin_amdgcn_perm(n > 3 ? d[3] & mask : 0u, d[2] & mask, sel) : 0u;
+    return (lo & 0xffffu) | hi << 16;
+  };
+  auto gather_codes = [&](int j) {  // of step j
+    const uint32_t mask = j < (K >> 7) ? 0xffffffffu : j == (K >> 7) ? tail_mask : 0u;
+#pragma unroll
+    for (int q = 0; q < QX; q++) cx[q] = gather(raw_x + 4 * q, TM - 4 * q, mask);
+#pragma unroll
+    for (int q = 0; q < QW; q++) cw[q] = gather(raw_w + 4 * q, TN - 4 * q, mask);
+  };
+
+  f32x4 acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; i++)
+#pragma unroll
+    for (int j = 0; j < TN; j++) acc[i][j] = (f32x4){0.f, 0.f, 0.f, 0.f};
+
+  // ---- K loop -----------------------------------------------------------------------------------------------------------
+  // Pairs of row blocks of X against the wave's fragments of W.  A pair's fragments are read one pair ahead; those of W for the
+  // next step during the last pair, each behind its last product.  Two barriers per step: behind the first the lower half
+  // of the stage's row blocks, W and codes have been read by all waves (their loads of two steps ahead go out there) and the upper
+  // half's loads have landed; behind the second the same the other way round, for the next step.  Every load so has one and
+  // a half steps to land.
+  using std::integral_constant;
+  constexpr int TP = TM / 2;
+  i32x8 fx[2][2], fw[TN];
+  auto product = [&](auto i_, auto j_, const i32x8 &x, int e) {
+    constexpr int i = decltype(i_)::value, j = decltype(j_)::value;
+    if constexpr (KIND == LIN_MX) {
+      acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[j], x, acc[i][j], 0, 0, j % 4, (int)cw[j / 4], i % 4, (int)cx[i / 4]);
+    } else {
+      const i32x8 &v = fw[j];
+      typedef int i32x4 __attribute__((ext_vector_type(4)));
+      const i32x4 wv = e ? __builtin_shufflevector(v, v, 4, 5, 6, 7) : __builtin_shufflevector(v, v, 0, 1, 2, 3);
+      const i32x4 xv = e ? __builtin_shufflevector(x, x, 4, 5, 6, 7) : __builtin_shufflevector(x, x, 0, 1, 2, 3);
+      acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wv), __builtin_bit_cast(bf16x8, xv), acc[i][j], 0, 0, 0);
+    }
+  };
+  issue_lo(0, 0);
+  issue_x(0, 0, integral_constant<int, 1>());
+  issue_lo(1, 1);
+  issue_x(1, 1, integral_constant<int, 1>());
+  wait_vmcnt<NHI + NLO + NHI>();
+  meet();
+  fx[0][0] = read_x(0);
+  fx[0][1] = read_x(1);
+#pragma unroll
+  for (int j = 0; j < TN; j++) fw[j] = read_w(j);
+  if constexpr (KIND == LIN_MX) {
+    read_codes();
+    gather_codes(0);
+  }
+  uint32_t st = 0;
+#pragma unroll 1
+  for (int kt = 0; kt < nk; kt++) {
+    auto pair = [&](auto p_) {
+      constexpr int p = decltype(p_)::value;
+      if constexpr (p < TP) {
+        if constexpr (p == TP / 2 - 1) {
+          __builtin_amdgcn_s_waitcnt(0xc07f);
+          wait_vmcnt<NLO + NHI>();  // (younger: the two parts of the next step)
+          meet();
+          issue_lo(st, kt + 2);
+        }
+        if constexpr (p == TP - 1) {
+          __builtin_amdgcn_s_waitcnt(0xc07f);
+          wait_vmcnt<NHI + NLO>();  // (younger: the next step's upper half, the lower part of the one behind)
+          meet();
+          issue_x(st, kt + 2, integral_constant<int, 1>());
+          const int da = st ? -A_BYTES : A_BYTES, db = st ? -B_BYTES : B_BYTES;
+          rx[0] += da;
+          rx[1] += da;
+#pragma unroll
+          for (int e = 0; e < NRW; e++) rw[e] += db;
+          if constexpr (KIND == LIN_MX) {
+            rs += st ? -S_BYTES : S_BYTES;
+            read_codes();
+          }
+        }
+        // (TP is even: pair p of every step uses set p % 2)
+        fx[(p + 1) & 1][0] = read_x(p < TP - 1 ? 2 * p + 2 : 0);
+        fx[(p + 1) & 1][1] = read_x(p < TP - 1 ? 2 * p + 3 : 1);
+        __builtin_amdgcn_sched_barrier(0);
+        auto column = [&](auto j_) {
+          constexpr int j = decltype(j_)::value;
+          if constexpr (j < TN) {
+#pragma unroll
+            for (int e = 0; e < (KIND == LIN_MX ? 1 : 2); e++) {
+              product(integral_constant<int, 2 * p>(), j_, fx[p & 1][0], e);
+              product(integral_constant<int, 2 * p + 1>(), j_, fx[p & 1][1], e);
+            }
+            if constexpr (p == TP - 1) {
+              __builtin_amdgcn_sched_barrier(0);
+              fw[j] = read_w(j);
+              __builtin_amdgcn_sched_barrier(0);
+            }
+          }
+        };
+        column(integral_constant<int, 0>()); column(integral_constant<int, 1>()); column(integral_constant<int, 2>()); column(integral_constant<int, 3>());
+        if constexpr (KIND == LIN_MX && p == TP - 1) gather_codes(kt + 1);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    pair(integral_constant<int, 0>()); pair(integral_constant<int, 1>()); pair(integral_constant<int, 2>()); pair(integral_constant<int, 3>());
+    st ^= 1;
+  }
+  wait_vmcnt<0>();  // (the zeros of the steps behind the last)
+  __builtin_amdgcn_s_waitcnt(0xc07f);
+  meet();
+
+  // ---- epilogue -----------------------------------------------------------------------------------------------------------
+  // Through LDS, 32 rows of the wave's tile at a time, so that a row's columns are stored as whole 16-byte packets side by side.
+  constexpr int LD = WTN + 4;  // floats
+  static_assert(NW * 32 * LD * 4 <= LDS_BYTES, "the epilogue's rows fit the stages");
+  float *tl = reinterpret_cast<float *>(lds) + w * 32 * LD;
+  constexpr int LPR = WTN / 8, RPP = 64 / LPR;  // lanes per row, rows per pass
+  const int er = lane / LPR, ec = (lane % LPR) * 8, n = n0 + wn * WTN + ec;
+  F8 bias;
+#pragma unroll
+  for (int i = 0; i < 8; i++) bias.v[i] = 0.0f;
+  if (a.bias && n < a.N) bias = load8(static_cast<const bf16_t *>(a.bias) + n);
+#pragma unroll
+  for (int i = 0; i < TM; i += 2) {
+#pragma unroll
+    for (int h = 0; h < 2; h++)
+#pragma unroll
+      for (int j = 0; j < TN; j++) *reinterpret_cast<f32x4 *>(tl + (16 * h + c) * LD + 16 * j + 4 * g) = acc[i + h][j];
+    // (a wave's own rows: its LDS operations complete in order)
+    asm volatile("" ::: "memory");
+    // a lane's rows of the pass: residuals first, all on their way together
+    constexpr int NP = 32 / RPP;
+    const int mi = m0 + wm * WTM + 16 * i + er;
+    Pkt res[NP], res2[NP];
+#pragma unroll
+    for (int p = 0; p < NP; p++) {
+      const size_t at = (size_t)min(mi + p * RPP, a.rows - 1) * a.N + min(n, a.N - 8);
+      if (a.R) res[p] = pkt_load(static_cast<const bf16_t *>(a.R) + at);
+      if (a.R2) res2[p] = pkt_load(static_cast<const bf16_t *>(a.R2) + at);
+    }
+#pragma unroll
+    for (int p = 0; p < NP; p++) {
+      const int m = mi + p * RPP;
+      F8 v = load8(tl + (p * RPP + er) * LD + ec);
+#pragma unroll
+      for (int e = 0; e < 8; e++) v.v[e] += bias.v[e];
+      activate<false>(v.v, a.act);
+      if (a.R) add8(v, res[p]);
+      if (a.R2) add8(v, res2[p]);
+      const bool in = m < a.rows && n < a.N;
+      const size_t at = (size_t)m * a.N + n;
+      if constexpr (MX_OUT) {  // N % 32 == 0: a quad's 32 columns are in or out together
+        u32x2 o;
+        const uint32_t code = mx_pack_quad(v, o);
+        if (in) *reinterpret_cast<u32x2 *>(static_cast<uint8_t *>(a.Y) + at) = o;
+        if (in && (lane & 3) == 0) {
+          uint8_t *s = a.Ys + (size_t)m * a.ys_stride + (n >> 5);
+          *s = (uint8_t)code;
+          if (n + 32 == a.N)  // the last block writes the padding's codes
+            for (int e = 1; (n >> 5) + e < a.ys_stride; e++) s[e] = 0;
+        }
+      } else if (in) {
+        store8(static_cast<bf16_t *>(a.Y) + at, v);
+      }
+    }
+    asm volatile("" ::: "memory");
+  }
+}
+
+template <int KIND, int BM, int BN, int WM, int WN>
+static void go(const LinArgs &a, bool mx_out, hipStream_t st) {
+  const int tm = (a.rows + BM - 1) / BM;
+  const int tn = (a.N + BN - 1) / BN;
+  const dim3 grid((unsigned)(tm * (long long)tn)), block(64 * WM * WN);
+  if constexpr (KIND == LIN_MX) {
+    if (mx_out) {
+      hipLaunchKernelGGL((k_linear_tile<KIND, BM, BN, WM, WN, true>), grid, block, 0, st, a, tm, tn);
+      return;
+    }
+  }
+  hipLaunchKernelGGL((k_linear_tile<KIND, BM, BN, WM, WN, false>), grid, block, 0, st, a, tm, tn);
+}
+
+int launch_linear_tile(int kind, const LinArgs &a, bool mx_out, hipStream_t st) {
+  KernelTimer kt(K_LINEAR, st);
+  const int which = getenv("LIN_TILE") ? atoi(getenv("LIN_TILE")) : 0;
+#define TILES(KIND) \
+  if (which == 0) go<KIND, 256, 256, 2, 4>(a, mx_out, st); \
+  else if (which == 1) go<KIND, 128, 128, 2, 2>(a, mx_out, st); \
+  else if (which == 2) go<KIND, 256, 128, 2, 2>(a, mx_out, st); \
+  else if (which == 4) go<KIND, 64, 64, 1, 2>(a, mx_out, st); \
+  else go<KIND, 64, 128, 1, 4>(a, mx_out, st);
+  if (kind == LIN_MX) { TILES(LIN_MX) } else { TILES(LIN_BF16) }
+  return launch_status();
+}
+
+}  // namespace toma

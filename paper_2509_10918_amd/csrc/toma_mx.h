@@ -55,6 +55,13 @@ __device__ __forceinline__ F8 load8(const float *p) {
   for (int i = 0; i < 4; i++) { o.v[i] = a[i]; o.v[4 + i] = b[i]; }
   return o;
 }
+__device__ __forceinline__ void add8(F8 &x, const Pkt &r) {  // eight bf16
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    x.v[2 * i] += __builtin_bit_cast(float, r.v[i] << 16);
+    x.v[2 * i + 1] += __builtin_bit_cast(float, r.v[i] & 0xffff0000u);
+  }
+}
 __device__ __forceinline__ void store8(bf16_t *p, const F8 &x) {
   bf16x8 o;
 #pragma unroll
