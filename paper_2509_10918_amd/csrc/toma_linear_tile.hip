@@ -35,11 +35,10 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a
   constexpr int NW = WM * WN, WTM = BM / WM, WTN = BN / WN, TM = WTM / 16, TN = WTN / 16;
   constexpr int ES = KIND == LIN_MX ? 1 : 2, BK = 128 / ES;
   constexpr int NIA = BM / 16 / NW, NIB = BN / 8 / NW;  // load instructions (1 KiB) per wave and step: half of X's rows, W
-  constexpr int NS = (BM + BN) / 64, NIS = KIND == LIN_MX ? (NS + NW - 1) / NW : 0;  // and the scale codes
-  constexpr int NLO = NIA + NIB + NIS, NHI = NIA;
+  constexpr int NS = (BM + BN) / 16, NIS = KIND == LIN_MX ? (NS + 4 * NW - 1) / (4 * NW) : 0;  // and a quarter of four steps' scale codes
   constexpr int PPR = BN / 8;                          // packets per k-row of a k-major stage
-  static_assert(NIA >= 1 && NIB >= 1 && TM >= 4 && TM % 4 == 0 && TN <= 4, "every wave loads its share");
-  constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, S_BYTES = KIND == LIN_MX ? (BM + BN) * 4 : 0;
+  static_assert(NIA >= 1 && NIB % 2 == 0 && TM >= 4 && TM % 4 == 0 && TN <= 4 && TN % (TM / 4) == 0, "every wave loads its share");
+  constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, S_BYTES = KIND == LIN_MX ? (BM + BN) * 16 : 0;
   constexpr int B_AT = 2 * A_BYTES, S_AT = B_AT + 2 * B_BYTES, LDS_BYTES = S_AT + 2 * S_BYTES;
   __shared__ __align__(1024) uint8_t lds[LDS_BYTES];
 
@@ -79,21 +78,26 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a
       wo[t] = (uint32_t)k * (uint32_t)(a.N * 2) + (uint32_t)min(p * 16, (a.N - n0 - 8) * 2);
     }
   }
-  // scale codes: a load instruction brings the four codes of 128 channels of 64 rows (of X, then of W)
+  // Scale codes come four steps (16 bytes a row) at a time, a quarter of the rows with every step: taken step by step, every load
+  // would fetch a cache line for four bytes, as many lines as all elements together.  A load instruction brings 16 rows, a
+  // lane's four bytes are those of one step.  Codes behind the end of a row repeat its last.
   const uint32_t l0 = lds_addr_of(lds);
-  const uint8_t *sb[NIS + 1];
-  uint32_t so[NIS + 1], ls[NIS + 1];
+  auto issue_codes = [&](int chunk, int part) {
 #pragma unroll
-  for (int t = 0; t < NIS; t++) {
-    const int sr = (w * NIS + t) % NS * 64;
-    const bool of_x = sr < BM;
-    sb[t] = of_x ? a.Xs + (size_t)m0 * a.xs_stride : a.Ws + (size_t)n0 * a.xs_stride;
-    so[t] = (uint32_t)min(sr + lane - (of_x ? 0 : BM), of_x ? a.rows - 1 - m0 : a.N - 1 - n0) * (uint32_t)a.xs_stride;
-    ls[t] = l0 + S_AT + (uint32_t)sr * 4;
-  }
+    for (int t = 0; t < NIS; t++) {
+      const int sr = ((part * NW + w) * NIS + t) % NS * 16;
+      const bool of_x = sr < BM;
+      const uint8_t *base = of_x ? a.Xs + (size_t)m0 * a.xs_stride : a.Ws + (size_t)n0 * a.xs_stride;
+      const int row = min(sr + (lane >> 2) - (of_x ? 0 : BM), of_x ? a.rows - 1 - m0 : a.N - 1 - n0);
+      const uint32_t off = (uint32_t)row * (uint32_t)a.xs_stride + (uint32_t)min(16 * chunk + 4 * (lane & 3), a.xs_stride - 4);
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(l0 + S_AT + (uint32_t)((chunk & 1) * S_BYTES + sr * 16)),
+                   "v"(off), "s"(base)
+                   : "memory", "m0");
+    }
+  };
 
-  // Loads of step j into its stage in two parts: W, codes and the lower half of X's row blocks, and the upper half.  Packets behind
-  // the end of K, and all of a step behind the last, are zeros that nothing is read for.
+  // Loads of a step into its stage: the lower and the upper half of X's row blocks, and W with the scale codes.  Packets behind the
+  // end of K, and all of a step behind the last, are zeros that nothing is read for.
   auto issue_x = [&](uint32_t st, int j, auto upper_) {
     constexpr int h = decltype(upper_)::value;
     const uint32_t bytes = j < nk ? 0x40000000u : 0u;
@@ -104,22 +108,15 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a
       buffer_to_lds16(xb + (size_t)j * 128, bytes, k < left ? xo[h][t] : kNoPacket, l0 + st * A_BYTES + (uint32_t)(x_row(t, h) * 128));
     }
   };
-  auto issue_lo = [&](uint32_t st, int j) {
-    if constexpr (KIND == LIN_MX) {
-#pragma unroll
-      for (int t = 0; t < NIS; t++)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(ls[t] + st * S_BYTES), "v"(so[t]),
-                     "s"(sb[t] + min(j, nk - 1) * 4)
-                     : "memory", "m0");
-    }
+  auto issue_w = [&](uint32_t st, int j, auto half_) {
+    constexpr int h = decltype(half_)::value;
     const uint32_t bytes = j < nk ? 0x40000000u : 0u;
     const int left = K - j * BK;
 #pragma unroll
-    for (int t = 0; t < NIB; t++) {
+    for (int t = h * (NIB / 2); t < (h + 1) * (NIB / 2); t++) {
       const int k = KIND == LIN_MX ? ((lane & 7) ^ ((((w * NIB + t) * 8 + (lane >> 3)) >> 1) & 7)) * 16 : (w * NIB + t) * (64 / PPR) + lane / PPR;
       buffer_to_lds16(wb + (size_t)j * w_step, bytes, k < left ? wo[t] : kNoPacket, l0 + B_AT + st * B_BYTES + (uint32_t)((w * NIB + t) * 1024));
     }
-    issue_x(st, j, std::integral_constant<int, 0>());
   };
   auto meet = [&]() {
     asm volatile("" ::: "memory");
@@ -133,7 +130,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a
   const int kq = 8 * g + (c >> 2), kcol = wn * WTN + 4 * (c & 3);  // (k-major weights: transpose reads)
   constexpr int NRW = KIND == LIN_MX ? 2 : TN;
   typedef __attribute__((address_space(3))) const uint8_t *lds_ptr;
-  lds_ptr rx[2], rw[NRW], rs = (lds_ptr)(lds + S_AT + c * 4);
+  lds_ptr rx[2], rw[NRW];
 #pragma unroll
   for (int e = 0; e < 2; e++) rx[e] = (lds_ptr)(lds + (wm * WTM + c) * 128 + (p0 ^ (64u * e)));
 #pragma unroll
@@ -163,11 +160,12 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a
   // scale codes of a step: byte b of word q is the code of row block 4 q + b for this lane's block of 32 channels (g)
   constexpr int QX = (TM + 3) / 4, QW = (TN + 3) / 4;
   uint32_t cx[QX], cw[QW], raw_x[TM], raw_w[TN];
-  auto read_codes = [&]() {
+  auto read_codes = [&](int j) {  // of step j
+    const lds_ptr at = (lds_ptr)(lds + S_AT) + ((j >> 2 & 1) * S_BYTES + (j & 3) * 4) + c * 16;
 #pragma unroll
-    for (int i = 0; i < TM; i++) raw_x[i] = *(lds_u32_ptr)(rs + (wm * WTM + 16 * i) * 4);
+    for (int i = 0; i < TM; i++) raw_x[i] = *(lds_u32_ptr)(at + (wm * WTM + 16 * i) * 16);
 #pragma unroll
-    for (int j = 0; j < TN; j++) raw_w[j] = *(lds_u32_ptr)(rs + (BM + wn * WTN + 16 * j) * 4);
+    for (int i = 0; i < TN; i++) raw_w[i] = *(lds_u32_ptr)(at + (BM + wn * WTN + 16 * i) * 16);
   };
   const uint32_t tail_mask = K % 128 ? 0xffffffffu >> (32 - (K >> 5) % 4 * 8) : 0u;  // codes of the last group that stand for channels
   auto gather = [&](const uint32_t *d, int n, uint32_t mask) {
@@ -191,94 +189,126 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a
     for (int j = 0; j < TN; j++) acc[i][j] = (f32x4){0.f, 0.f, 0.f, 0.f};
 
   // ---- K loop -----------------------------------------------------------------------------------------------------------
-  // Pairs of row blocks of X against the wave's fragments of W.  A pair's fragments are read one pair ahead; those of W for the
-  // next step during the last pair, each behind its last product.  Two barriers per step: behind the first the lower half
-  // of the stage's row blocks, W and codes have been read by all waves (their loads of two steps ahead go out there) and the upper
-  // half's loads have landed; behind the second the same the other way round, for the next step.  Every load so has one and
-  // a half steps to land.
+  // A step goes through TP pairs of row blocks of X, each in two phases: memory (the pair's fragments from LDS, in the second half
+  // of the pairs those of W and the codes for the next step, and loads) and products.  With eight waves the two waves of a SIMD take
+  // turns: a barrier stands behind every phase, and waves 4 .. 7 run one phase behind, so that one wave of a SIMD feeds the
+  // matrix core while the other one waits for memory.  (Both in the same phase at the same time, the matrix cores were busy 53 % of
+  // the time: 8192^3 in 8 bits 506 us.)  With four waves two workgroups share a CU and take turns by themselves.
+  // What a phase may read or overwrite (s: step): X's lower pairs are read in the first half of the pairs, so in the second half
+  // their place takes the loads of step s + 2; the upper pairs, and W of step s + 1, in the second half: in the step behind, their
+  // places take the loads of the upper pairs of step s + 2 and W of step s + 3.  The loads are spread over the phases (28 at once
+  // kept the address unit busy for longer than a phase).  A wave waits for its loads of a half before the barrier in front of that
+  // half; every load has a step or more to land.
   using std::integral_constant;
-  constexpr int TP = TM / 2;
-  i32x8 fx[2][2], fw[TN];
-  auto product = [&](auto i_, auto j_, const i32x8 &x, int e) {
+  constexpr int TP = TM / 2, HP = TP / 2;
+  constexpr bool TURNS = NW == 8;
+  i32x8 fx[2], fw[2][TN];
+  auto product = [&](auto i_, auto j_, const i32x8 &x, const i32x8 &v, int e) {
     constexpr int i = decltype(i_)::value, j = decltype(j_)::value;
     if constexpr (KIND == LIN_MX) {
-      acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[j], x, acc[i][j], 0, 0, j % 4, (int)cw[j / 4], i % 4, (int)cx[i / 4]);
+      acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(v, x, acc[i][j], 0, 0, j % 4, (int)cw[j / 4], i % 4, (int)cx[i / 4]);
     } else {
-      const i32x8 &v = fw[j];
       typedef int i32x4 __attribute__((ext_vector_type(4)));
       const i32x4 wv = e ? __builtin_shufflevector(v, v, 4, 5, 6, 7) : __builtin_shufflevector(v, v, 0, 1, 2, 3);
       const i32x4 xv = e ? __builtin_shufflevector(x, x, 4, 5, 6, 7) : __builtin_shufflevector(x, x, 0, 1, 2, 3);
       acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wv), __builtin_bit_cast(bf16x8, xv), acc[i][j], 0, 0, 0);
     }
   };
-  issue_lo(0, 0);
-  issue_x(0, 0, integral_constant<int, 1>());
-  issue_lo(1, 1);
-  issue_x(1, 1, integral_constant<int, 1>());
-  wait_vmcnt<NHI + NLO + NHI>();
-  meet();
-  fx[0][0] = read_x(0);
-  fx[0][1] = read_x(1);
-#pragma unroll
-  for (int j = 0; j < TN; j++) fw[j] = read_w(j);
+  constexpr integral_constant<int, 0> lower{};
+  constexpr integral_constant<int, 1> upper{};
+  auto next_codes = [&](int j) {  // with the loads of step j: the codes of a chunk are complete with those of its first step
+    if constexpr (KIND == LIN_MX) issue_codes(((j - 1) >> 2) + 1, (j - 1) & 3);
+  };
   if constexpr (KIND == LIN_MX) {
-    read_codes();
+    issue_codes(0, 0);
+    issue_codes(0, 1);
+    issue_codes(0, 2);
+  }
+  next_codes(0);
+  issue_w(0, 0, lower);
+  issue_w(0, 0, upper);
+  issue_x(0, 0, lower);
+  issue_x(0, 0, upper);
+  next_codes(1);
+  issue_w(1, 1, lower);
+  issue_w(1, 1, upper);
+  issue_x(1, 1, lower);
+  wait_vmcnt<2 * NIA + NIB + NIS>();  // W and the lower half of step 0
+  meet();
+#pragma unroll
+  for (int j = 0; j < TN; j++) fw[0][j] = read_w(j);
+  if constexpr (KIND == LIN_MX) {
+    read_codes(0);
     gather_codes(0);
   }
-  uint32_t st = 0;
-#pragma unroll 1
-  for (int kt = 0; kt < nk; kt++) {
+#pragma unroll
+  for (int e = 0; e < NRW; e++) rw[e] += B_BYTES;
+  __builtin_amdgcn_s_waitcnt(0xc07f);
+  meet();  // every wave has W of step 0
+  if (TURNS && w >= 4) meet();
+  auto step = [&](auto st_, int kt) {
+    constexpr int st = decltype(st_)::value;
     auto pair = [&](auto p_) {
       constexpr int p = decltype(p_)::value;
       if constexpr (p < TP) {
-        if constexpr (p == TP / 2 - 1) {
-          __builtin_amdgcn_s_waitcnt(0xc07f);
-          wait_vmcnt<NLO + NHI>();  // (younger: the two parts of the next step)
-          meet();
-          issue_lo(st, kt + 2);
+        fx[0] = read_x(2 * p);
+        fx[1] = read_x(2 * p + 1);
+        if constexpr (p >= HP) {
+#pragma unroll
+          for (int j = 0; j < TN; j++)
+            if (j / (TN / HP) == p - HP) fw[st ^ 1][j] = read_w(j);
+          if constexpr (KIND == LIN_MX && p == TP - 1) read_codes(kt + 1);
         }
-        if constexpr (p == TP - 1) {
-          __builtin_amdgcn_s_waitcnt(0xc07f);
-          wait_vmcnt<NHI + NLO>();  // (younger: the next step's upper half, the lower part of the one behind)
-          meet();
-          issue_x(st, kt + 2, integral_constant<int, 1>());
-          const int da = st ? -A_BYTES : A_BYTES, db = st ? -B_BYTES : B_BYTES;
+        if constexpr (p == 0) {
+          issue_x(st ^ 1, kt + 1, upper);
+          next_codes(kt + 2);
+        }
+        if constexpr (p == HP - 1) issue_w(st, kt + 2, lower);
+        if constexpr (p == HP) issue_w(st, kt + 2, upper);
+        if constexpr (p == TP - 1) issue_x(st, kt + 2, lower);
+        if constexpr (p == TP - 1) {  // the addresses move to the other stage
+          constexpr int da = st ? -A_BYTES : A_BYTES, db = st ? B_BYTES : -B_BYTES;
           rx[0] += da;
           rx[1] += da;
 #pragma unroll
           for (int e = 0; e < NRW; e++) rw[e] += db;
-          if constexpr (KIND == LIN_MX) {
-            rs += st ? -S_BYTES : S_BYTES;
-            read_codes();
-          }
         }
-        // (TP is even: pair p of every step uses set p % 2)
-        fx[(p + 1) & 1][0] = read_x(p < TP - 1 ? 2 * p + 2 : 0);
-        fx[(p + 1) & 1][1] = read_x(p < TP - 1 ? 2 * p + 3 : 1);
         __builtin_amdgcn_sched_barrier(0);
+        if constexpr (TURNS || p == HP - 1 || p == TP - 1) {
+          __builtin_amdgcn_s_waitcnt(0xc07f);
+          if constexpr (p == HP - 1) wait_vmcnt<2 * NIA + NIS + NIB / 2>();
+          if constexpr (p == TP - 1) wait_vmcnt<2 * NIA + NIS + NIB>();
+          meet();
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
         auto column = [&](auto j_) {
           constexpr int j = decltype(j_)::value;
           if constexpr (j < TN) {
 #pragma unroll
             for (int e = 0; e < (KIND == LIN_MX ? 1 : 2); e++) {
-              product(integral_constant<int, 2 * p>(), j_, fx[p & 1][0], e);
-              product(integral_constant<int, 2 * p + 1>(), j_, fx[p & 1][1], e);
-            }
-            if constexpr (p == TP - 1) {
-              __builtin_amdgcn_sched_barrier(0);
-              fw[j] = read_w(j);
-              __builtin_amdgcn_sched_barrier(0);
+              product(integral_constant<int, 2 * p>(), j_, fx[0], fw[st][j], e);
+              product(integral_constant<int, 2 * p + 1>(), j_, fx[1], fw[st][j], e);
             }
           }
         };
         column(integral_constant<int, 0>()); column(integral_constant<int, 1>()); column(integral_constant<int, 2>()); column(integral_constant<int, 3>());
+        __builtin_amdgcn_s_setprio(0);
+        __builtin_amdgcn_sched_barrier(0);
         if constexpr (KIND == LIN_MX && p == TP - 1) gather_codes(kt + 1);
+        if constexpr (TURNS) meet();
         __builtin_amdgcn_sched_barrier(0);
       }
     };
     pair(integral_constant<int, 0>()); pair(integral_constant<int, 1>()); pair(integral_constant<int, 2>()); pair(integral_constant<int, 3>());
-    st ^= 1;
+  };
+  for (int kt = 0;;) {
+    step(lower, kt);
+    if (++kt >= nk) break;
+    step(upper, kt);
+    if (++kt >= nk) break;
   }
+  if (TURNS && w < 4) meet();
   wait_vmcnt<0>();  // (the zeros of the steps behind the last)
   __builtin_amdgcn_s_waitcnt(0xc07f);
   meet();
