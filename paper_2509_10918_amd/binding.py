@@ -264,22 +264,38 @@ _TYPE = {torch.float32: TOMA_F32, torch.bfloat16: TOMA_BF16, "f32": TOMA_F32, "b
 _TORCH = {TOMA_F32: torch.float32, TOMA_BF16: torch.bfloat16, TOMA_MX8: torch.uint8}
 
 
-def _arg(what, t, code, count):
-    """Pointer of a tensor argument after its checks; count: elements it has to hold."""
-    if t is None:
-        return None
-    if t.dtype != _TORCH[code] or t.numel() != count:
-        raise ValueError(f"{what}: {count} elements of {_TORCH[code]} expected, got {t.numel()} of {t.dtype}")
+def _refuse(what, t, dtype, count, device):
+    if t.dtype is not dtype or t.numel() != count:
+        raise ValueError(f"{what}: {count} elements of {dtype} expected, got {t.numel()} of {t.dtype}")
     if not (t.is_cuda and t.is_contiguous()):
         raise ValueError(f"{what}: libtoma takes contiguous CUDA tensors")
-    if t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"{what} lies on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
-    return t.data_ptr()
+    raise ValueError(f"{what} lies on {t.device}, the current device is cuda:{device}")
 
 
-def _scratch(ws):
-    """Pointer and bytes of a scratch tensor (None: no scratch)."""
-    return (None, 0) if ws is None else (_arg("ws", ws, TOMA_MX8, ws.numel()), ws.numel())
+class _Call:
+    """Pointers of one call's tensor arguments after their checks, and the current stream.  (A small call's time is the host's: the
+    device and the stream are asked for once per call.)"""
+
+    __slots__ = ("device",)
+
+    def __init__(self):
+        self.device = torch.cuda.current_device() if torch.cuda.is_initialized() else 0
+
+    def arg(self, what, t, code, count):
+        """count: elements the tensor has to hold."""
+        if t is None:
+            return None
+        dtype = _TORCH[code]
+        if t.dtype is not dtype or t.numel() != count or t.get_device() != self.device or not t.is_contiguous():
+            _refuse(what, t, dtype, count, self.device)
+        return t.data_ptr()
+
+    def scratch(self, ws):
+        """Pointer and bytes of a scratch tensor (None: no scratch)."""
+        return (None, 0) if ws is None else (self.arg("ws", ws, TOMA_MX8, ws.numel()), ws.numel())
+
+    def stream(self):
+        return torch._C._cuda_getCurrentRawStream(self.device)
 
 
 def _scale_stride(K):
@@ -299,28 +315,30 @@ def alloc_mx(rows, K, device="cuda"):
             torch.empty((rows, stride), dtype=torch.uint8, device=device))
 
 
+def _pack_call(name, plain, code, rows, K, lead, Q, S):
+    c = _Call()
+    p = c.arg("Y" if name == "toma_mx_dequantize" else "W" if name == "toma_mx_quantize_weight" else "X", plain, max(code, 0), rows * K)
+    q, s = c.arg("Q", Q, TOMA_MX8, rows * K), c.arg("S", S, TOMA_MX8, rows * _scale_stride(K))
+    args = (q, s, p) if name == "toma_mx_dequantize" else (p, q, s)
+    _check(getattr(lib(), name)(code, *lead, *args, c.stream()), name)
+
+
 def toma_mx_quantize(X, Q, S):
     """X [..., K] -> Q [rows, K], S [rows, stride] (alloc_mx)."""
     rows, K = Q.shape
-    code = _TYPE.get(X.dtype, -1)
-    _check(lib().toma_mx_quantize(code, rows, K, _arg("X", X, max(code, 0), rows * K), _arg("Q", Q, TOMA_MX8, rows * K),
-                                  _arg("S", S, TOMA_MX8, rows * _scale_stride(K)), _stream()), "toma_mx_quantize")
+    _pack_call("toma_mx_quantize", X, _TYPE.get(X.dtype, -1), rows, K, (rows, K), Q, S)
 
 
 def toma_mx_quantize_weight(W, Q, S):
     """W [K, N] -> Q [N, K], S [N, stride] (alloc_mx(N, K))."""
     K, N = W.shape
-    code = _TYPE.get(W.dtype, -1)
-    _check(lib().toma_mx_quantize_weight(code, K, N, _arg("W", W, max(code, 0), K * N), _arg("Q", Q, TOMA_MX8, K * N),
-                                         _arg("S", S, TOMA_MX8, N * _scale_stride(K)), _stream()), "toma_mx_quantize_weight")
+    _pack_call("toma_mx_quantize_weight", W, _TYPE.get(W.dtype, -1), N, K, (K, N), Q, S)
 
 
 def toma_mx_dequantize(Q, S, Y):
     """The values of Q [rows, K], S as Y [..., K] (float32 or bfloat16)."""
     rows, K = Q.shape
-    code = _TYPE.get(Y.dtype, -1)
-    _check(lib().toma_mx_dequantize(code, rows, K, _arg("Q", Q, TOMA_MX8, rows * K), _arg("S", S, TOMA_MX8, rows * _scale_stride(K)),
-                                    _arg("Y", Y, max(code, 0), rows * K), _stream()), "toma_mx_dequantize")
+    _pack_call("toma_mx_dequantize", Y, _TYPE.get(Y.dtype, -1), rows, K, (rows, K), Q, S)
 
 
 def make_norm_desc(rows, C, eps, x_type, y_type=None):
@@ -328,9 +346,10 @@ def make_norm_desc(rows, C, eps, x_type, y_type=None):
 
 
 def toma_rmsnorm(desc, X, R, gamma, H, Y, Ys=None):
-    n, x = desc.rows * desc.C, desc.x_type
-    _check(lib().toma_rmsnorm(_ref(desc), _arg("X", X, x, n), _arg("R", R, x, n), _arg("gamma", gamma, x, desc.C), _arg("H", H, x, n),
-                              _arg("Y", Y, desc.y_type, n), _arg("Ys", Ys, TOMA_MX8, desc.rows * _scale_stride(desc.C)), _stream()),
+    rows, C, x = desc.rows, desc.C, desc.x_type
+    n, c = rows * C, _Call()
+    _check(lib().toma_rmsnorm(_ref(desc), c.arg("X", X, x, n), c.arg("R", R, x, n), c.arg("gamma", gamma, x, C), c.arg("H", H, x, n),
+                              c.arg("Y", Y, desc.y_type, n), c.arg("Ys", Ys, TOMA_MX8, rows * _scale_stride(C)), c.stream()),
            "toma_rmsnorm")
 
 
@@ -354,10 +373,10 @@ def alloc_linear_workspace(desc, device="cuda"):
 def toma_linear(desc, X, Xs, W, Ws, bias, R, Y, Ys, ws):
     rows, K, N, x = desc.rows, desc.K, desc.N, desc.x_type
     e = TOMA_F32 if x == TOMA_F32 else TOMA_BF16   # bias and residual
-    p, n = _scratch(ws)
-    _check(lib().toma_linear(_ref(desc), _arg("X", X, x, rows * K), _arg("Xs", Xs, TOMA_MX8, rows * _scale_stride(K)), _arg("W", W, x, K * N),
-                             _arg("Ws", Ws, TOMA_MX8, N * _scale_stride(K)), _arg("bias", bias, e, N), _arg("R", R, e, rows * N),
-                             _arg("Y", Y, desc.y_type, rows * N), _arg("Ys", Ys, TOMA_MX8, rows * _scale_stride(N)), p, n, _stream()),
+    c = _Call()
+    _check(lib().toma_linear(_ref(desc), c.arg("X", X, x, rows * K), c.arg("Xs", Xs, TOMA_MX8, rows * _scale_stride(K)), c.arg("W", W, x, K * N),
+                             c.arg("Ws", Ws, TOMA_MX8, N * _scale_stride(K)), c.arg("bias", bias, e, N), c.arg("R", R, e, rows * N),
+                             c.arg("Y", Y, desc.y_type, rows * N), c.arg("Ys", Ys, TOMA_MX8, rows * _scale_stride(N)), *c.scratch(ws), c.stream()),
            "toma_linear")
 
 
@@ -377,11 +396,11 @@ def alloc_ffn_workspace(desc, device="cuda"):
 
 
 def toma_ffn(desc, X, R, gamma, W1, W1s, b1, W2, W2s, b2, Y, ws):
-    n, C, hidden, x, w = desc.rows * desc.C, desc.C, desc.hidden, desc.x_type, desc.w_type
-    p, nb = _scratch(ws)
-    _check(lib().toma_ffn(_ref(desc), _arg("X", X, x, n), _arg("R", R, x, n), _arg("gamma", gamma, x, C), _arg("W1", W1, w, C * hidden),
-                          _arg("W1s", W1s, TOMA_MX8, hidden * _scale_stride(C)), _arg("b1", b1, x, hidden), _arg("W2", W2, w, C * hidden),
-                          _arg("W2s", W2s, TOMA_MX8, C * _scale_stride(hidden)), _arg("b2", b2, x, C), _arg("Y", Y, x, n), p, nb, _stream()),
+    C, hidden, x, w = desc.C, desc.hidden, desc.x_type, desc.w_type
+    n, c = desc.rows * C, _Call()
+    _check(lib().toma_ffn(_ref(desc), c.arg("X", X, x, n), c.arg("R", R, x, n), c.arg("gamma", gamma, x, C), c.arg("W1", W1, w, C * hidden),
+                          c.arg("W1s", W1s, TOMA_MX8, hidden * _scale_stride(C)), c.arg("b1", b1, x, hidden), c.arg("W2", W2, w, C * hidden),
+                          c.arg("W2s", W2s, TOMA_MX8, C * _scale_stride(hidden)), c.arg("b2", b2, x, C), c.arg("Y", Y, x, n), *c.scratch(ws), c.stream()),
            "toma_ffn")
 
 

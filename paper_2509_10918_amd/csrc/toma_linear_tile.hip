@@ -30,16 +30,19 @@ template <int PPR> __device__ __forceinline__ int km_place(int k, int pi) {
   return pi ^ (((k >> 1) & 1) << 2) ^ (((k >> 3) & 1) << 1);
 }
 
-template <int KIND, int BM, int BN, int WM, int WN, bool MX_OUT>
-__global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a, int tiles_m, int tiles_n) {
+template <int KIND, int BM, int BN, int WM, int WN, int STAGES, bool MX_OUT>
+__global__ __launch_bounds__(64 * WM * WN, STAGES * (BM + BN) > 640 ? 1 : 2) void k_linear_tile(const LinArgs a, int tiles_m, int tiles_n) {
   constexpr int NW = WM * WN, WTM = BM / WM, WTN = BN / WN, TM = WTM / 16, TN = WTN / 16;
   constexpr int ES = KIND == LIN_MX ? 1 : 2, BK = 128 / ES;
   constexpr int NIA = BM / 16 / NW, NIB = BN / 8 / NW;  // load instructions (1 KiB) per wave and step: half of X's rows, W
   constexpr int NS = (BM + BN) / 16, NIS = KIND == LIN_MX ? (NS + 4 * NW - 1) / (4 * NW) : 0;  // and a quarter of four steps' scale codes
   constexpr int PPR = BN / 8;                          // packets per k-row of a k-major stage
-  static_assert(NIA >= 1 && NIB % 2 == 0 && TM >= 4 && TM % 4 == 0 && TN <= 4 && TN % (TM / 4) == 0, "every wave loads its share");
+  static_assert(NIA >= 1 && NIB >= 1, "every wave loads its share");
+  static_assert(STAGES > 2 ? TM % 2 == 0 : TM % 4 == 0 && NIB % 2 == 0 && TN % (TM / 4) == 0, "row blocks in pairs and halves");
+  static_assert(TN <= 4 && TM <= 8, "column and row blocks spelled out below");
   constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, S_BYTES = KIND == LIN_MX ? (BM + BN) * 16 : 0;
-  constexpr int B_AT = 2 * A_BYTES, S_AT = B_AT + 2 * B_BYTES, LDS_BYTES = S_AT + 2 * S_BYTES;
+  constexpr int SLOTS = (STAGES + 9) / 4;  // of four steps' codes: a slot takes its next codes STAGES + 6 steps after its first were read
+  constexpr int B_AT = STAGES * A_BYTES, S_AT = B_AT + STAGES * B_BYTES, LDS_BYTES = S_AT + SLOTS * S_BYTES;
   __shared__ __align__(1024) uint8_t lds[LDS_BYTES];
 
   int tile_m, tile_n;
@@ -90,7 +93,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a
       const uint8_t *base = of_x ? a.Xs + (size_t)m0 * a.xs_stride : a.Ws + (size_t)n0 * a.xs_stride;
       const int row = min(sr + (lane >> 2) - (of_x ? 0 : BM), of_x ? a.rows - 1 - m0 : a.N - 1 - n0);
       const uint32_t off = (uint32_t)row * (uint32_t)a.xs_stride + (uint32_t)min(16 * chunk + 4 * (lane & 3), a.xs_stride - 4);
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(l0 + S_AT + (uint32_t)((chunk & 1) * S_BYTES + sr * 16)),
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(l0 + S_AT + (uint32_t)(chunk % SLOTS * S_BYTES + sr * 16)),
                    "v"(off), "s"(base)
                    : "memory", "m0");
     }
@@ -113,7 +116,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a
     const uint32_t bytes = j < nk ? 0x40000000u : 0u;
     const int left = K - j * BK;
 #pragma unroll
-    for (int t = h * (NIB / 2); t < (h + 1) * (NIB / 2); t++) {
+    for (int t = h * NIB / 2; t < (h + 1) * NIB / 2; t++) {
       const int k = KIND == LIN_MX ? ((lane & 7) ^ ((((w * NIB + t) * 8 + (lane >> 3)) >> 1) & 7)) * 16 : (w * NIB + t) * (64 / PPR) + lane / PPR;
       buffer_to_lds16(wb + (size_t)j * w_step, bytes, k < left ? wo[t] : kNoPacket, l0 + B_AT + st * B_BYTES + (uint32_t)((w * NIB + t) * 1024));
     }
@@ -142,16 +145,16 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a
   typedef __attribute__((address_space(3))) const uint32_t *lds_u32_ptr;
   typedef s16x4 __attribute__((address_space(3))) *lds_s16x4_ptr;
   auto join = [](u32x4 a, u32x4 b) { return __builtin_bit_cast(i32x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7)); };
-  auto read_x = [&](int i) { return join(*(lds_u32x4_ptr)(rx[0] + i * 2048), *(lds_u32x4_ptr)(rx[1] + i * 2048)); };
-  auto read_w = [&](int j) {
+  auto read_x = [&](int i, int at = 0) { return join(*(lds_u32x4_ptr)(rx[0] + at + i * 2048), *(lds_u32x4_ptr)(rx[1] + at + i * 2048)); };
+  auto read_w = [&](int j, int at = 0) {
     if constexpr (KIND == LIN_MX) {
-      return join(*(lds_u32x4_ptr)(rw[0] + j * 2048), *(lds_u32x4_ptr)(rw[1] + j * 2048));
+      return join(*(lds_u32x4_ptr)(rw[0] + at + j * 2048), *(lds_u32x4_ptr)(rw[1] + at + j * 2048));
     } else {
       u32x4 f[2];
 #pragma unroll
       for (int e = 0; e < 2; e++) {
-        const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(rw[j] + 32 * e * PPR * 16)));
-        const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(rw[j] + (32 * e + 4) * PPR * 16)));
+        const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(rw[j] + at + 32 * e * PPR * 16)));
+        const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(rw[j] + at + (32 * e + 4) * PPR * 16)));
         f[e] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3);
       }
       return join(f[0], f[1]);
@@ -161,7 +164,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a
   constexpr int QX = (TM + 3) / 4, QW = (TN + 3) / 4;
   uint32_t cx[QX], cw[QW], raw_x[TM], raw_w[TN];
   auto read_codes = [&](int j) {  // of step j
-    const lds_ptr at = (lds_ptr)(lds + S_AT) + ((j >> 2 & 1) * S_BYTES + (j & 3) * 4) + c * 16;
+    const lds_ptr at = (lds_ptr)(lds + S_AT) + ((j >> 2) % SLOTS * S_BYTES + (j & 3) * 4) + c * 16;
 #pragma unroll
     for (int i = 0; i < TM; i++) raw_x[i] = *(lds_u32_ptr)(at + (wm * WTM + 16 * i) * 16);
 #pragma unroll
@@ -189,20 +192,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a
     for (int j = 0; j < TN; j++) acc[i][j] = (f32x4){0.f, 0.f, 0.f, 0.f};
 
   // ---- K loop -----------------------------------------------------------------------------------------------------------
-  // A step goes through TP pairs of row blocks of X, each in two phases: memory (the pair's fragments from LDS, in the second half
-  // of the pairs those of W and the codes for the next step, and loads) and products.  With eight waves the two waves of a SIMD take
-  // turns: a barrier stands behind every phase, and waves 4 .. 7 run one phase behind, so that one wave of a SIMD feeds the
-  // matrix core while the other one waits for memory.  (Both in the same phase at the same time, the matrix cores were busy 53 % of
-  // the time: 8192^3 in 8 bits 506 us.)  With four waves two workgroups share a CU and take turns by themselves.
-  // What a phase may read or overwrite (s: step): X's lower pairs are read in the first half of the pairs, so in the second half
-  // their place takes the loads of step s + 2; the upper pairs, and W of step s + 1, in the second half: in the step behind, their
-  // places take the loads of the upper pairs of step s + 2 and W of step s + 3.  The loads are spread over the phases (28 at once
-  // kept the address unit busy for longer than a phase).  A wave waits for its loads of a half before the barrier in front of that
-  // half; every load has a step or more to land.
   using std::integral_constant;
-  constexpr int TP = TM / 2, HP = TP / 2;
-  constexpr bool TURNS = NW == 8;
-  i32x8 fx[2], fw[2][TN];
+  constexpr bool TURNS = STAGES == 2 && NW == 8;
   auto product = [&](auto i_, auto j_, const i32x8 &x, const i32x8 &v, int e) {
     constexpr int i = decltype(i_)::value, j = decltype(j_)::value;
     if constexpr (KIND == LIN_MX) {
@@ -219,6 +210,19 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a
   auto next_codes = [&](int j) {  // with the loads of step j: the codes of a chunk are complete with those of its first step
     if constexpr (KIND == LIN_MX) issue_codes(((j - 1) >> 2) + 1, (j - 1) & 3);
   };
+  if constexpr (STAGES == 2) {
+  // A step goes through TP pairs of row blocks of X, each in two phases: memory (the pair's fragments from LDS, in the second half
+  // of the pairs those of W and the codes for the next step, and loads) and products.  With eight waves the two waves of a SIMD take
+  // turns: a barrier stands behind every phase, and waves 4 .. 7 run one phase behind, so that one wave of a SIMD feeds the
+  // matrix core while the other one waits for memory.  (Both in the same phase at the same time, the matrix cores were busy 53 % of
+  // the time: 8192^3 in 8 bits 506 us.)  With four waves two workgroups share a CU and take turns by themselves.
+  // What a phase may read or overwrite (s: step): X's lower pairs are read in the first half of the pairs, so in the second half
+  // their place takes the loads of step s + 2; the upper pairs, and W of step s + 1, in the second half: in the step behind, their
+  // places take the loads of the upper pairs of step s + 2 and W of step s + 3.  The loads are spread over the phases (28 at once
+  // kept the address unit busy for longer than a phase).  A wave waits for its loads of a half before the barrier in front of that
+  // half; every load has a step or more to land.
+  constexpr int TP = TM / 2, HP = TP / 2;
+  i32x8 fx[2], fw[2][TN];
   if constexpr (KIND == LIN_MX) {
     issue_codes(0, 0);
     issue_codes(0, 1);
@@ -308,6 +312,80 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a
     step(upper, kt);
     if (++kt >= nk) break;
   }
+  } else {
+  // Small tiles: one step's fragments are read while the products of the step before run, one barrier per step, loads STAGES steps
+  // ahead (a stage is free once its fragments have been read).  What counts here is how long one step takes: few workgroups, each
+  // with a chain of K steps.
+  constexpr int L = 2 * NIA + NIB + NIS;  // loads of a step
+  auto issue = [&](uint32_t st, int j) {
+    next_codes(j);
+    issue_w(st, j, lower);
+    issue_w(st, j, upper);
+    issue_x(st, j, lower);
+    issue_x(st, j, upper);
+  };
+  if constexpr (KIND == LIN_MX) {
+    issue_codes(0, 0);
+    issue_codes(0, 1);
+    issue_codes(0, 2);
+  }
+#pragma unroll
+  for (int t = 0; t < STAGES; t++) issue(t, t);
+  i32x8 fx[2][TM], fw[2][TN];
+  auto read = [&](auto set_, int st, int j) {
+    constexpr int set = decltype(set_)::value;
+#pragma unroll
+    for (int i = 0; i < TM; i++) fx[set][i] = read_x(i, st * A_BYTES);
+#pragma unroll
+    for (int i = 0; i < TN; i++) fw[set][i] = read_w(i, st * B_BYTES);
+    if constexpr (KIND == LIN_MX) read_codes(j);
+  };
+  wait_vmcnt<(STAGES - 1) * L>();
+  meet();
+  read(lower, 0, 0);
+  if constexpr (KIND == LIN_MX) gather_codes(0);
+  __builtin_amdgcn_s_waitcnt(0xc07f);
+  wait_vmcnt<(STAGES - 2) * L>();
+  meet();
+  int st = 0;
+  auto step = [&](auto set_, int kt) {
+    constexpr int set = decltype(set_)::value;
+    const int nst = st + 1 == STAGES ? 0 : st + 1;
+    read(integral_constant<int, set ^ 1>(), nst, kt + 1);
+    issue(st, kt + STAGES);
+    __builtin_amdgcn_sched_barrier(0);
+    auto row = [&](auto i_) {
+      constexpr int i = decltype(i_)::value;
+      auto column = [&](auto j_, int e) {
+        constexpr int j = decltype(j_)::value;
+        if constexpr (i < TM && j < TN) product(i_, j_, fx[set][i], fw[set][j], e);
+      };
+#pragma unroll
+      for (int e = 0; e < (KIND == LIN_MX ? 1 : 2); e++) {
+        column(integral_constant<int, 0>(), e);
+        column(integral_constant<int, 1>(), e);
+        column(integral_constant<int, 2>(), e);
+        column(integral_constant<int, 3>(), e);
+      }
+    };
+    row(integral_constant<int, 0>());
+    row(integral_constant<int, 1>());
+    row(integral_constant<int, 2>());
+    row(integral_constant<int, 3>());
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (KIND == LIN_MX) gather_codes(kt + 1);
+    __builtin_amdgcn_s_waitcnt(0xc07f);
+    wait_vmcnt<(STAGES - 2) * L>();  // step kt + 2 has landed
+    meet();
+    st = nst;
+  };
+  for (int kt = 0;;) {
+    step(lower, kt);
+    if (++kt >= nk) break;
+    step(upper, kt);
+    if (++kt >= nk) break;
+  }
+  }
   if (TURNS && w < 4) meet();
   wait_vmcnt<0>();  // (the zeros of the steps behind the last)
   __builtin_amdgcn_s_waitcnt(0xc07f);
@@ -371,29 +449,31 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a
   }
 }
 
-template <int KIND, int BM, int BN, int WM, int WN>
+template <int KIND, int BM, int BN, int WM, int WN, int STAGES>
 static void go(const LinArgs &a, bool mx_out, hipStream_t st) {
   const int tm = (a.rows + BM - 1) / BM;
   const int tn = (a.N + BN - 1) / BN;
   const dim3 grid((unsigned)(tm * (long long)tn)), block(64 * WM * WN);
   if constexpr (KIND == LIN_MX) {
     if (mx_out) {
-      hipLaunchKernelGGL((k_linear_tile<KIND, BM, BN, WM, WN, true>), grid, block, 0, st, a, tm, tn);
+      hipLaunchKernelGGL((k_linear_tile<KIND, BM, BN, WM, WN, STAGES, true>), grid, block, 0, st, a, tm, tn);
       return;
     }
   }
-  hipLaunchKernelGGL((k_linear_tile<KIND, BM, BN, WM, WN, false>), grid, block, 0, st, a, tm, tn);
+  hipLaunchKernelGGL((k_linear_tile<KIND, BM, BN, WM, WN, STAGES, false>), grid, block, 0, st, a, tm, tn);
 }
 
 int launch_linear_tile(int kind, const LinArgs &a, bool mx_out, hipStream_t st) {
   KernelTimer kt(K_LINEAR, st);
   const int which = getenv("LIN_TILE") ? atoi(getenv("LIN_TILE")) : 0;
 #define TILES(KIND) \
-  if (which == 0) go<KIND, 256, 256, 2, 4>(a, mx_out, st); \
-  else if (which == 1) go<KIND, 128, 128, 2, 2>(a, mx_out, st); \
-  else if (which == 2) go<KIND, 256, 128, 2, 2>(a, mx_out, st); \
-  else if (which == 4) go<KIND, 64, 64, 1, 2>(a, mx_out, st); \
-  else go<KIND, 64, 128, 1, 4>(a, mx_out, st);
+  if (which == 0) go<KIND, 256, 256, 2, 4, 2>(a, mx_out, st); \
+  else if (which == 1) go<KIND, 128, 128, 2, 2, 4>(a, mx_out, st); \
+  else if (which == 2) go<KIND, 128, 64, 2, 2, 3>(a, mx_out, st); \
+  else if (which == 3) go<KIND, 64, 128, 2, 2, 6>(a, mx_out, st); \
+  else if (which == 4) go<KIND, 64, 64, 2, 2, 4>(a, mx_out, st); \
+  else if (which == 5) go<KIND, 128, 128, 2, 2, 2>(a, mx_out, st); \
+  else go<KIND, 64, 64, 2, 2, 8>(a, mx_out, st);
   if (kind == LIN_MX) { TILES(LIN_MX) } else { TILES(LIN_BF16) }
   return launch_status();
 }
