@@ -68,6 +68,117 @@ __device__ __forceinline__ void tile_of(int id, int total, int tiles_m, int tile
   tm = 8 * grp + in - tn * high;
 }
 
+enum { LIN_BF16 = 0, LIN_MX = 1 };
+
+constexpr uint32_t kNoPacket = 0x80000000u;  // lane offset of a packet that is not there: zeros (tiles span less than 2^30 bytes)
+constexpr uint32_t kAllPackets = 0x40000000u;
+typedef __attribute__((address_space(3))) const uint8_t *lds_ptr;
+typedef __attribute__((address_space(3))) const u32x4 *lds_u32x4_ptr;
+typedef __attribute__((address_space(3))) const u32x2 *lds_u32x2_ptr;
+typedef __attribute__((address_space(3))) const uint32_t *lds_u32_ptr;
+typedef s16x4 __attribute__((address_space(3))) *lds_s16x4_ptr;
+
+// One load-to-LDS instruction through a buffer descriptor: lane l's 16 bytes at base + off land at lds_addr + 16 l, zeros for a lane
+// whose offset is kNoPacket or beyond `bytes` (base, bytes, lds_addr: uniform).
+__device__ __forceinline__ u32x4 buffer_of(const uint8_t *base, uint32_t bytes) {
+  const uint64_t b = (uint64_t)base;
+  return (u32x4){(uint32_t)b, (uint32_t)(b >> 32), bytes, 0x00020000u};
+}
+__device__ __forceinline__ void buffer_to_lds16(const uint8_t *base, uint32_t bytes, uint32_t off, uint32_t lds_addr) {
+  const u32x4 rsrc = buffer_of(base, bytes);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds_addr), "v"(off), "s"(rsrc) : "memory", "m0");
+}
+// workgroup barrier that the compiler may not move memory accesses across
+__device__ __forceinline__ void meet() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ i32x8 join_halves(u32x4 a, u32x4 b) {
+  return __builtin_bit_cast(i32x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+// half e of a bf16 fragment pair
+__device__ __forceinline__ bf16x8 bf16_half(const i32x8 &v, int e) {
+  typedef int i32x4 __attribute__((ext_vector_type(4)));
+  const i32x4 h = e ? __builtin_shufflevector(v, v, 4, 5, 6, 7) : __builtin_shufflevector(v, v, 0, 1, 2, 3);
+  return __builtin_bit_cast(bf16x8, h);
+}
+// byte g of d[0 .. n - 1] (masked) as the bytes of one word
+__device__ __forceinline__ uint32_t gather_bytes(const uint32_t *d, int n, uint32_t mask, int g) {
+  const uint32_t sel = (uint32_t)g | (uint32_t)(4 + g) << 8;  // byte g of the second, then of the first operand
+  const uint32_t lo = __builtin_amdgcn_perm(n > 1 ? d[1] & mask : 0u, d[0] & mask, sel);
+  const uint32_t hi = n > 2 ? __builtin_amdgcn_perm(n > 3 ? d[3] & mask : 0u, d[2] & mask, sel) : 0u;
+  return (lo & 0xffffu) | hi << 16;
+}
+// place of packet pi of k-row k in a k-major stage of PPR packets a row: four rows of 32 bytes that a transpose read takes together
+// fall on the four quarters of 256 bytes, the rows eight further on (the upper half of the wave) on what they leave
+template <int PPR> __device__ __forceinline__ int km_place(int k, int pi) {
+  if constexpr (PPR >= 16) return pi ^ ((k & 3) << 2) ^ (((k >> 3) & 1) << 1);
+  return pi ^ (((k >> 1) & 1) << 2) ^ (((k >> 3) & 1) << 1);
+}
+
+// Epilogue of a wave's tile of TM x TN accumulators (lane: row 16 i + lane % 16, columns 16 j + 4 (lane / 16) + r) at (m_w, n_w).
+// Through LDS (tl: kEpilogueFloats of the wave's own), 32 rows at a time, so that a row's columns are stored as whole 16-byte
+// packets side by side.
+template <int TN> constexpr int kEpilogueFloats = 32 * (16 * TN + 4);
+template <int TM, int TN, bool MX_OUT>
+__device__ __forceinline__ void linear_epilogue(const LinArgs &a, const f32x4 (&acc)[TM][TN], float *tl, int m_w, int n_w, int lane) {
+  constexpr int LD = 16 * TN + 4;               // floats
+  constexpr int LPR = 2 * TN, RPP = 64 / LPR;   // lanes per row, rows per pass
+  const int g = lane >> 4, c = lane & 15, er = lane / LPR, ec = (lane % LPR) * 8, n = n_w + ec;
+  F8 bias;
+#pragma unroll
+  for (int i = 0; i < 8; i++) bias.v[i] = 0.0f;
+  if (a.bias && n < a.N) bias = load8(static_cast<const bf16_t *>(a.bias) + n);
+#pragma unroll
+  for (int i = 0; i < TM; i += 2) {
+#pragma unroll
+    for (int h = 0; h < 2; h++)
+#pragma unroll
+      for (int j = 0; j < TN; j++) *reinterpret_cast<f32x4 *>(tl + (16 * h + c) * LD + 16 * j + 4 * g) = acc[i + h][j];
+    // (a wave's own rows: its LDS operations complete in order)
+    asm volatile("" ::: "memory");
+    // a lane's rows of the pass: residuals first, all on their way together
+    constexpr int NP = 32 / RPP;
+    const int mi = m_w + 16 * i + er;
+    Pkt res[NP], res2[NP];
+#pragma unroll
+    for (int p = 0; p < NP; p++) {
+      const size_t at = (size_t)min(mi + p * RPP, a.rows - 1) * a.N + min(n, a.N - 8);
+      if (a.R) res[p] = pkt_load(static_cast<const bf16_t *>(a.R) + at);
+      if (a.R2) res2[p] = pkt_load(static_cast<const bf16_t *>(a.R2) + at);
+    }
+#pragma unroll
+    for (int p = 0; p < NP; p++) {
+      const int m = mi + p * RPP;
+      F8 v = load8(tl + (p * RPP + er) * LD + ec);
+#pragma unroll
+      for (int e = 0; e < 8; e++) v.v[e] += bias.v[e];
+      activate<false>(v.v, a.act);
+      if (a.R) add8(v, res[p]);
+      if (a.R2) add8(v, res2[p]);
+      const bool in = m < a.rows && n < a.N;
+      const size_t at = (size_t)m * a.N + n;
+      if constexpr (MX_OUT) {  // N % 32 == 0: a quad's 32 columns are in or out together
+        u32x2 o;
+        const uint32_t code = mx_pack_quad(v, o);
+        if (in) *reinterpret_cast<u32x2 *>(static_cast<uint8_t *>(a.Y) + at) = o;
+        if (in && (lane & 3) == 0) {
+          uint8_t *s = a.Ys + (size_t)m * a.ys_stride + (n >> 5);
+          *s = (uint8_t)code;
+          if (n + 32 == a.N)  // the last block writes the padding's codes
+            for (int e = 1; (n >> 5) + e < a.ys_stride; e++) s[e] = 0;
+        }
+      } else if (in) {
+        store8(static_cast<bf16_t *>(a.Y) + at, v);
+      }
+    }
+    asm volatile("" ::: "memory");
+  }
+}
+
+// Both launch without a timer of their own.
+int launch_linear_small(int kind, int bm, int bn, const LinArgs &a, bool mx_out, hipStream_t st);
 int launch_linear_tile(int kind, const LinArgs &a, bool mx_out, hipStream_t st);
 
 }  // namespace toma

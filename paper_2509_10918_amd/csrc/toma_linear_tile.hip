@@ -12,37 +12,19 @@
 
 namespace toma {
 
-enum { LIN_BF16 = 0, LIN_MX = 1 };
-
-// One load-to-LDS instruction through a buffer descriptor: lane l's 16 bytes at base + off land at lds_addr + 16 l, zeros for a lane
-// whose offset is kNoPacket or beyond `bytes` (both uniform).
-constexpr uint32_t kNoPacket = 0x80000000u;  // (tiles span less than 2^30 bytes)
-__device__ __forceinline__ void buffer_to_lds16(const uint8_t *base, uint32_t bytes, uint32_t off, uint32_t lds_addr) {
-  const uint64_t b = (uint64_t)base;
-  const u32x4 rsrc = {(uint32_t)b, (uint32_t)(b >> 32), bytes, 0x00020000u};
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds_addr), "v"(off), "s"(rsrc) : "memory", "m0");
-}
-
-// place of packet pi of k-row k in a k-major stage of PPR packets a row: four rows of 32 bytes that a transpose read takes together
-// fall on the four quarters of 256 bytes, the rows eight further on (the upper half of the wave) on what they leave
-template <int PPR> __device__ __forceinline__ int km_place(int k, int pi) {
-  if constexpr (PPR >= 16) return pi ^ ((k & 3) << 2) ^ (((k >> 3) & 1) << 1);
-  return pi ^ (((k >> 1) & 1) << 2) ^ (((k >> 3) & 1) << 1);
-}
-
-template <int KIND, int BM, int BN, int WM, int WN, int STAGES, bool MX_OUT>
-__global__ __launch_bounds__(64 * WM * WN, STAGES * (BM + BN) > 640 ? 1 : 2) void k_linear_tile(const LinArgs a, int tiles_m, int tiles_n) {
+template <int KIND, int BM, int BN, int WM, int WN, bool MX_OUT>
+__global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a, int tiles_m, int tiles_n) {
   constexpr int NW = WM * WN, WTM = BM / WM, WTN = BN / WN, TM = WTM / 16, TN = WTN / 16;
   constexpr int ES = KIND == LIN_MX ? 1 : 2, BK = 128 / ES;
   constexpr int NIA = BM / 16 / NW, NIB = BN / 8 / NW;  // load instructions (1 KiB) per wave and step: half of X's rows, W
   constexpr int NS = (BM + BN) / 16, NIS = KIND == LIN_MX ? (NS + 4 * NW - 1) / (4 * NW) : 0;  // and a quarter of four steps' scale codes
   constexpr int PPR = BN / 8;                          // packets per k-row of a k-major stage
   static_assert(NIA >= 1 && NIB >= 1, "every wave loads its share");
-  static_assert(STAGES > 2 ? TM % 2 == 0 : TM % 4 == 0 && NIB % 2 == 0 && TN % (TM / 4) == 0, "row blocks in pairs and halves");
+  static_assert(TM % 4 == 0 && NIB % 2 == 0 && TN % (TM / 4) == 0, "row blocks in pairs and halves");
   static_assert(TN <= 4 && TM <= 8, "column and row blocks spelled out below");
   constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, S_BYTES = KIND == LIN_MX ? (BM + BN) * 16 : 0;
-  constexpr int SLOTS = (STAGES + 9) / 4;  // of four steps' codes: a slot takes its next codes STAGES + 6 steps after its first were read
-  constexpr int B_AT = STAGES * A_BYTES, S_AT = B_AT + STAGES * B_BYTES, LDS_BYTES = S_AT + SLOTS * S_BYTES;
+  constexpr int SLOTS = 2;  // of four steps' codes
+  constexpr int B_AT = 2 * A_BYTES, S_AT = B_AT + 2 * B_BYTES, LDS_BYTES = S_AT + SLOTS * S_BYTES;
   __shared__ __align__(1024) uint8_t lds[LDS_BYTES];
 
   int tile_m, tile_n;
@@ -121,18 +103,11 @@ __global__ __launch_bounds__(64 * WM * WN, STAGES * (BM + BN) > 640 ? 1 : 2) voi
       buffer_to_lds16(wb + (size_t)j * w_step, bytes, k < left ? wo[t] : kNoPacket, l0 + B_AT + st * B_BYTES + (uint32_t)((w * NIB + t) * 1024));
     }
   };
-  auto meet = [&]() {
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-  };
-
   // ---- fragments: a lane takes packets g and 4 + g of its row (bf16: one of each half of the step) ------------------------
   // LDS addresses of the stage that is read; they move to the other stage at the end of a step
   const uint32_t p0 = (uint32_t)(g ^ ((c >> 1) & 7)) << 4;
   const int kq = 8 * g + (c >> 2), kcol = wn * WTN + 4 * (c & 3);  // (k-major weights: transpose reads)
   constexpr int NRW = KIND == LIN_MX ? 2 : TN;
-  typedef __attribute__((address_space(3))) const uint8_t *lds_ptr;
   lds_ptr rx[2], rw[NRW];
 #pragma unroll
   for (int e = 0; e < 2; e++) rx[e] = (lds_ptr)(lds + (wm * WTM + c) * 128 + (p0 ^ (64u * e)));
@@ -141,23 +116,19 @@ __global__ __launch_bounds__(64 * WM * WN, STAGES * (BM + BN) > 640 ? 1 : 2) voi
     if constexpr (KIND == LIN_MX) rw[e] = (lds_ptr)(lds + B_AT + (wn * WTN + c) * 128 + (p0 ^ (64u * e)));
     else rw[e] = (lds_ptr)(lds + B_AT + (kq * PPR + km_place<PPR>(kq, (kcol + 16 * e) >> 3)) * 16 + (kcol & 7) * 2);
   }
-  typedef __attribute__((address_space(3))) const u32x4 *lds_u32x4_ptr;
-  typedef __attribute__((address_space(3))) const uint32_t *lds_u32_ptr;
-  typedef s16x4 __attribute__((address_space(3))) *lds_s16x4_ptr;
-  auto join = [](u32x4 a, u32x4 b) { return __builtin_bit_cast(i32x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7)); };
-  auto read_x = [&](int i, int at = 0) { return join(*(lds_u32x4_ptr)(rx[0] + at + i * 2048), *(lds_u32x4_ptr)(rx[1] + at + i * 2048)); };
-  auto read_w = [&](int j, int at = 0) {
+  auto read_x = [&](int i) { return join_halves(*(lds_u32x4_ptr)(rx[0] + i * 2048), *(lds_u32x4_ptr)(rx[1] + i * 2048)); };
+  auto read_w = [&](int j) {
     if constexpr (KIND == LIN_MX) {
-      return join(*(lds_u32x4_ptr)(rw[0] + at + j * 2048), *(lds_u32x4_ptr)(rw[1] + at + j * 2048));
+      return join_halves(*(lds_u32x4_ptr)(rw[0] + j * 2048), *(lds_u32x4_ptr)(rw[1] + j * 2048));
     } else {
       u32x4 f[2];
 #pragma unroll
       for (int e = 0; e < 2; e++) {
-        const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(rw[j] + at + 32 * e * PPR * 16)));
-        const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(rw[j] + at + (32 * e + 4) * PPR * 16)));
+        const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(rw[j] + 32 * e * PPR * 16)));
+        const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(rw[j] + (32 * e + 4) * PPR * 16)));
         f[e] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3);
       }
-      return join(f[0], f[1]);
+      return join_halves(f[0], f[1]);
     }
   };
   // scale codes of a step: byte b of word q is the code of row block 4 q + b for this lane's block of 32 channels (g)
@@ -171,18 +142,12 @@ __global__ __launch_bounds__(64 * WM * WN, STAGES * (BM + BN) > 640 ? 1 : 2) voi
     for (int i = 0; i < TN; i++) raw_w[i] = *(lds_u32_ptr)(at + (BM + wn * WTN + 16 * i) * 16);
   };
   const uint32_t tail_mask = K % 128 ? 0xffffffffu >> (32 - (K >> 5) % 4 * 8) : 0u;  // codes of the last group that stand for channels
-  auto gather = [&](const uint32_t *d, int n, uint32_t mask) {
-    const uint32_t sel = (uint32_t)g | (uint32_t)(4 + g) << 8;  // byte g of the second, then of the first operand
-    const uint32_t lo = __builtin_amdgcn_perm(n > 1 ? d[1] & mask : 0u, d[0] & mask, sel);
-    const uint32_t hi = n > 2 ? __builtin_amdgcn_perm(n > 3 ? d[3] & mask : 0u, d[2] & mask, sel) : 0u;
-    return (lo & 0xffffu) | hi << 16;
-  };
   auto gather_codes = [&](int j) {  // of step j
     const uint32_t mask = j < (K >> 7) ? 0xffffffffu : j == (K >> 7) ? tail_mask : 0u;
 #pragma unroll
-    for (int q = 0; q < QX; q++) cx[q] = gather(raw_x + 4 * q, TM - 4 * q, mask);
+    for (int q = 0; q < QX; q++) cx[q] = gather_bytes(raw_x + 4 * q, TM - 4 * q, mask, g);
 #pragma unroll
-    for (int q = 0; q < QW; q++) cw[q] = gather(raw_w + 4 * q, TN - 4 * q, mask);
+    for (int q = 0; q < QW; q++) cw[q] = gather_bytes(raw_w + 4 * q, TN - 4 * q, mask, g);
   };
 
   f32x4 acc[TM][TN];
@@ -193,16 +158,13 @@ __global__ __launch_bounds__(64 * WM * WN, STAGES * (BM + BN) > 640 ? 1 : 2) voi
 
   // ---- K loop -----------------------------------------------------------------------------------------------------------
   using std::integral_constant;
-  constexpr bool TURNS = STAGES == 2 && NW == 8;
+  constexpr bool TURNS = NW == 8;
   auto product = [&](auto i_, auto j_, const i32x8 &x, const i32x8 &v, int e) {
     constexpr int i = decltype(i_)::value, j = decltype(j_)::value;
     if constexpr (KIND == LIN_MX) {
       acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(v, x, acc[i][j], 0, 0, j % 4, (int)cw[j / 4], i % 4, (int)cx[i / 4]);
     } else {
-      typedef int i32x4 __attribute__((ext_vector_type(4)));
-      const i32x4 wv = e ? __builtin_shufflevector(v, v, 4, 5, 6, 7) : __builtin_shufflevector(v, v, 0, 1, 2, 3);
-      const i32x4 xv = e ? __builtin_shufflevector(x, x, 4, 5, 6, 7) : __builtin_shufflevector(x, x, 0, 1, 2, 3);
-      acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wv), __builtin_bit_cast(bf16x8, xv), acc[i][j], 0, 0, 0);
+      acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_half(v, e), bf16_half(x, e), acc[i][j], 0, 0, 0);
     }
   };
   constexpr integral_constant<int, 0> lower{};
@@ -210,7 +172,6 @@ __global__ __launch_bounds__(64 * WM * WN, STAGES * (BM + BN) > 640 ? 1 : 2) voi
   auto next_codes = [&](int j) {  // with the loads of step j: the codes of a chunk are complete with those of its first step
     if constexpr (KIND == LIN_MX) issue_codes(((j - 1) >> 2) + 1, (j - 1) & 3);
   };
-  if constexpr (STAGES == 2) {
   // A step goes through TP pairs of row blocks of X, each in two phases: memory (the pair's fragments from LDS, in the second half
   // of the pairs those of W and the codes for the next step, and loads) and products.  With eight waves the two waves of a SIMD take
   // turns: a barrier stands behind every phase, and waves 4 .. 7 run one phase behind, so that one wave of a SIMD feeds the
@@ -312,168 +273,35 @@ __global__ __launch_bounds__(64 * WM * WN, STAGES * (BM + BN) > 640 ? 1 : 2) voi
     step(upper, kt);
     if (++kt >= nk) break;
   }
-  } else {
-  // Small tiles: one step's fragments are read while the products of the step before run, one barrier per step, loads STAGES steps
-  // ahead (a stage is free once its fragments have been read).  What counts here is how long one step takes: few workgroups, each
-  // with a chain of K steps.
-  constexpr int L = 2 * NIA + NIB + NIS;  // loads of a step
-  auto issue = [&](uint32_t st, int j) {
-    next_codes(j);
-    issue_w(st, j, lower);
-    issue_w(st, j, upper);
-    issue_x(st, j, lower);
-    issue_x(st, j, upper);
-  };
-  if constexpr (KIND == LIN_MX) {
-    issue_codes(0, 0);
-    issue_codes(0, 1);
-    issue_codes(0, 2);
-  }
-#pragma unroll
-  for (int t = 0; t < STAGES; t++) issue(t, t);
-  i32x8 fx[2][TM], fw[2][TN];
-  auto read = [&](auto set_, int st, int j) {
-    constexpr int set = decltype(set_)::value;
-#pragma unroll
-    for (int i = 0; i < TM; i++) fx[set][i] = read_x(i, st * A_BYTES);
-#pragma unroll
-    for (int i = 0; i < TN; i++) fw[set][i] = read_w(i, st * B_BYTES);
-    if constexpr (KIND == LIN_MX) read_codes(j);
-  };
-  wait_vmcnt<(STAGES - 1) * L>();
-  meet();
-  read(lower, 0, 0);
-  if constexpr (KIND == LIN_MX) gather_codes(0);
-  __builtin_amdgcn_s_waitcnt(0xc07f);
-  wait_vmcnt<(STAGES - 2) * L>();
-  meet();
-  int st = 0;
-  auto step = [&](auto set_, int kt) {
-    constexpr int set = decltype(set_)::value;
-    const int nst = st + 1 == STAGES ? 0 : st + 1;
-    read(integral_constant<int, set ^ 1>(), nst, kt + 1);
-    issue(st, kt + STAGES);
-    __builtin_amdgcn_sched_barrier(0);
-    auto row = [&](auto i_) {
-      constexpr int i = decltype(i_)::value;
-      auto column = [&](auto j_, int e) {
-        constexpr int j = decltype(j_)::value;
-        if constexpr (i < TM && j < TN) product(i_, j_, fx[set][i], fw[set][j], e);
-      };
-#pragma unroll
-      for (int e = 0; e < (KIND == LIN_MX ? 1 : 2); e++) {
-        column(integral_constant<int, 0>(), e);
-        column(integral_constant<int, 1>(), e);
-        column(integral_constant<int, 2>(), e);
-        column(integral_constant<int, 3>(), e);
-      }
-    };
-    row(integral_constant<int, 0>());
-    row(integral_constant<int, 1>());
-    row(integral_constant<int, 2>());
-    row(integral_constant<int, 3>());
-    __builtin_amdgcn_sched_barrier(0);
-    if constexpr (KIND == LIN_MX) gather_codes(kt + 1);
-    __builtin_amdgcn_s_waitcnt(0xc07f);
-    wait_vmcnt<(STAGES - 2) * L>();  // step kt + 2 has landed
-    meet();
-    st = nst;
-  };
-  for (int kt = 0;;) {
-    step(lower, kt);
-    if (++kt >= nk) break;
-    step(upper, kt);
-    if (++kt >= nk) break;
-  }
-  }
   if (TURNS && w < 4) meet();
   wait_vmcnt<0>();  // (the zeros of the steps behind the last)
   __builtin_amdgcn_s_waitcnt(0xc07f);
   meet();
 
-  // ---- epilogue -----------------------------------------------------------------------------------------------------------
-  // Through LDS, 32 rows of the wave's tile at a time, so that a row's columns are stored as whole 16-byte packets side by side.
-  constexpr int LD = WTN + 4;  // floats
-  static_assert(NW * 32 * LD * 4 <= LDS_BYTES, "the epilogue's rows fit the stages");
-  float *tl = reinterpret_cast<float *>(lds) + w * 32 * LD;
-  constexpr int LPR = WTN / 8, RPP = 64 / LPR;  // lanes per row, rows per pass
-  const int er = lane / LPR, ec = (lane % LPR) * 8, n = n0 + wn * WTN + ec;
-  F8 bias;
-#pragma unroll
-  for (int i = 0; i < 8; i++) bias.v[i] = 0.0f;
-  if (a.bias && n < a.N) bias = load8(static_cast<const bf16_t *>(a.bias) + n);
-#pragma unroll
-  for (int i = 0; i < TM; i += 2) {
-#pragma unroll
-    for (int h = 0; h < 2; h++)
-#pragma unroll
-      for (int j = 0; j < TN; j++) *reinterpret_cast<f32x4 *>(tl + (16 * h + c) * LD + 16 * j + 4 * g) = acc[i + h][j];
-    // (a wave's own rows: its LDS operations complete in order)
-    asm volatile("" ::: "memory");
-    // a lane's rows of the pass: residuals first, all on their way together
-    constexpr int NP = 32 / RPP;
-    const int mi = m0 + wm * WTM + 16 * i + er;
-    Pkt res[NP], res2[NP];
-#pragma unroll
-    for (int p = 0; p < NP; p++) {
-      const size_t at = (size_t)min(mi + p * RPP, a.rows - 1) * a.N + min(n, a.N - 8);
-      if (a.R) res[p] = pkt_load(static_cast<const bf16_t *>(a.R) + at);
-      if (a.R2) res2[p] = pkt_load(static_cast<const bf16_t *>(a.R2) + at);
-    }
-#pragma unroll
-    for (int p = 0; p < NP; p++) {
-      const int m = mi + p * RPP;
-      F8 v = load8(tl + (p * RPP + er) * LD + ec);
-#pragma unroll
-      for (int e = 0; e < 8; e++) v.v[e] += bias.v[e];
-      activate<false>(v.v, a.act);
-      if (a.R) add8(v, res[p]);
-      if (a.R2) add8(v, res2[p]);
-      const bool in = m < a.rows && n < a.N;
-      const size_t at = (size_t)m * a.N + n;
-      if constexpr (MX_OUT) {  // N % 32 == 0: a quad's 32 columns are in or out together
-        u32x2 o;
-        const uint32_t code = mx_pack_quad(v, o);
-        if (in) *reinterpret_cast<u32x2 *>(static_cast<uint8_t *>(a.Y) + at) = o;
-        if (in && (lane & 3) == 0) {
-          uint8_t *s = a.Ys + (size_t)m * a.ys_stride + (n >> 5);
-          *s = (uint8_t)code;
-          if (n + 32 == a.N)  // the last block writes the padding's codes
-            for (int e = 1; (n >> 5) + e < a.ys_stride; e++) s[e] = 0;
-        }
-      } else if (in) {
-        store8(static_cast<bf16_t *>(a.Y) + at, v);
-      }
-    }
-    asm volatile("" ::: "memory");
-  }
+  linear_epilogue<TM, TN, MX_OUT>(a, acc, reinterpret_cast<float *>(lds) + w * kEpilogueFloats<TN>, m0 + wm * WTM, n0 + wn * WTN, lane);
 }
 
-template <int KIND, int BM, int BN, int WM, int WN, int STAGES>
+template <int KIND, int BM, int BN, int WM, int WN>
 static void go(const LinArgs &a, bool mx_out, hipStream_t st) {
   const int tm = (a.rows + BM - 1) / BM;
   const int tn = (a.N + BN - 1) / BN;
   const dim3 grid((unsigned)(tm * (long long)tn)), block(64 * WM * WN);
   if constexpr (KIND == LIN_MX) {
     if (mx_out) {
-      hipLaunchKernelGGL((k_linear_tile<KIND, BM, BN, WM, WN, STAGES, true>), grid, block, 0, st, a, tm, tn);
+      hipLaunchKernelGGL((k_linear_tile<KIND, BM, BN, WM, WN, true>), grid, block, 0, st, a, tm, tn);
       return;
     }
   }
-  hipLaunchKernelGGL((k_linear_tile<KIND, BM, BN, WM, WN, STAGES, false>), grid, block, 0, st, a, tm, tn);
+  hipLaunchKernelGGL((k_linear_tile<KIND, BM, BN, WM, WN, false>), grid, block, 0, st, a, tm, tn);
 }
 
 int launch_linear_tile(int kind, const LinArgs &a, bool mx_out, hipStream_t st) {
   KernelTimer kt(K_LINEAR, st);
   const int which = getenv("LIN_TILE") ? atoi(getenv("LIN_TILE")) : 0;
+  if (which >= 2) return launch_linear_small(kind, which, 0, a, mx_out, st);
 #define TILES(KIND) \
-  if (which == 0) go<KIND, 256, 256, 2, 4, 2>(a, mx_out, st); \
-  else if (which == 1) go<KIND, 128, 128, 2, 2, 4>(a, mx_out, st); \
-  else if (which == 2) go<KIND, 128, 64, 2, 2, 3>(a, mx_out, st); \
-  else if (which == 3) go<KIND, 64, 128, 2, 2, 6>(a, mx_out, st); \
-  else if (which == 4) go<KIND, 64, 64, 2, 2, 4>(a, mx_out, st); \
-  else if (which == 5) go<KIND, 128, 128, 2, 2, 2>(a, mx_out, st); \
-  else go<KIND, 64, 64, 2, 2, 8>(a, mx_out, st);
+  if (which == 0) go<KIND, 256, 256, 2, 4>(a, mx_out, st); \
+  else go<KIND, 128, 128, 2, 2>(a, mx_out, st);
   if (kind == LIN_MX) { TILES(LIN_MX) } else { TILES(LIN_BF16) }
   return launch_status();
 }
