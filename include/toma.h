@@ -353,8 +353,8 @@ int toma_linear(const toma_linear_desc *desc, const void *X, const void *Xs_opt,
  *   gamma_opt     [C];  b1_opt [hidden];  b2_opt [C]     x_type
  *   W1 [C, hidden], W2 [hidden, C]  in x_type; w_type TOMA_MX8 (x_type TOMA_BF16 only): [hidden, C] and [C, hidden] packed
  *                 by toma_mx_quantize_weight, with their scale codes
- *   h and everything between lies in ws (toma_ffn_workspace_bytes, 256-byte aligned)
- * Between the stages the norm's output, the hidden values and h are rounded to x_type (w_type TOMA_MX8: the first two packed).
+ *   everything between lies in ws (toma_ffn_workspace_bytes, 256-byte aligned)
+ * Between the stages the norm's output and the hidden values are rounded to x_type (w_type TOMA_MX8: packed); h is not rounded.
  * Limits: C % 32 == 0, C <= 16384, hidden % 32 == 0; sizes as for toma_linear.
  */
 typedef struct {

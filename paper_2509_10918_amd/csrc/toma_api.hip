@@ -524,14 +524,14 @@ TOMA_API int toma_linear(const toma_linear_desc *desc, const void *X, const void
     if (misaligned(ws, 256)) return TOMA_ERR_ALIGN;
     if (ws_bytes < need) return TOMA_ERR_WORKSPACE;
   }
-  return launch_linear(*desc, X, Xs_opt, W, Ws_opt, bias_opt, R_opt, Y, Ys_opt, ws, static_cast<hipStream_t>(stream));
+  return launch_linear(*desc, X, Xs_opt, W, Ws_opt, bias_opt, R_opt, nullptr, Y, Ys_opt, ws, static_cast<hipStream_t>(stream));
 }
 
 // The stages of a feed-forward block and where their outputs lie in the workspace.
 struct FfnPlan {
   toma_norm_desc norm;
   toma_linear_desc up, down;
-  size_t h, n, ns, u, us, lin, total;
+  size_t n, ns, u, us, lin, total;
 };
 static int plan_ffn(const toma_ffn_desc *d, FfnPlan *p) {
   if (!d) return TOMA_ERR_NULL;
@@ -548,7 +548,6 @@ static int plan_ffn(const toma_ffn_desc *d, FfnPlan *p) {
   const size_t rows = (size_t)d->rows, es = d->x_type == TOMA_F32 ? 4 : 2, ew = mx ? 1 : es;
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t o = off; off += up256(bytes); return o; };
-  p->h = take(rows * d->C * es);
   p->n = take(rows * d->C * ew);
   p->ns = take(mx ? rows * mx_scale_stride(d->C) : 0);
   p->u = take(rows * d->hidden * ew);
@@ -578,10 +577,11 @@ TOMA_API int toma_ffn(const toma_ffn_desc *desc, const void *X, const void *R_op
   if (ws_bytes < p.total) return TOMA_ERR_WORKSPACE;
   hipStream_t st = static_cast<hipStream_t>(stream);
   char *wsb = static_cast<char *>(ws);
-  void *h = R_opt ? static_cast<void *>(wsb + p.h) : nullptr, *ns = mx ? wsb + p.ns : nullptr, *us = mx ? wsb + p.us : nullptr;
-  rc = launch_rmsnorm(p.norm, X, R_opt, gamma_opt, h, wsb + p.n, ns, st);
+  void *ns = mx ? wsb + p.ns : nullptr, *us = mx ? wsb + p.us : nullptr;
+  rc = launch_rmsnorm(p.norm, X, R_opt, gamma_opt, nullptr, wsb + p.n, ns, st);
   if (rc != TOMA_OK) return rc;
-  rc = launch_linear(p.up, wsb + p.n, ns, W1, W1s_opt, b1_opt, nullptr, wsb + p.u, us, wsb + p.lin, st);
+  rc = launch_linear(p.up, wsb + p.n, ns, W1, W1s_opt, b1_opt, nullptr, nullptr, wsb + p.u, us, wsb + p.lin, st);
   if (rc != TOMA_OK) return rc;
-  return launch_linear(p.down, wsb + p.u, us, W2, W2s_opt, b2_opt, h ? h : X, Y, nullptr, wsb + p.lin, st);
+  // (h is not stored: the last epilogue adds X and R again, unrounded, for the bytes that writing and reading h would take)
+  return launch_linear(p.down, wsb + p.u, us, W2, W2s_opt, b2_opt, X, R_opt, Y, nullptr, wsb + p.lin, st);
 }

@@ -177,8 +177,8 @@ __device__ __forceinline__ void linear_epilogue(const LinArgs &a, const f32x4 (&
   }
 }
 
-// Both launch without a timer of their own.
-int launch_linear_small(int kind, int bm, int bn, const LinArgs &a, bool mx_out, hipStream_t st);
-int launch_linear_tile(int kind, const LinArgs &a, bool mx_out, hipStream_t st);
+// part: fp32 scratch [nsplit][rows][N] when nsplit > 1
+void launch_linear_small(const LinArgs &a, bool mx_out, int nsplit, float *part, hipStream_t st);
+void launch_linear_tile(int kind, bool large, const LinArgs &a, bool mx_out, hipStream_t st);
 
 }  // namespace toma

@@ -1,9 +1,10 @@
-// Products of the linear layer with few output tiles: bf16, and 8 bits with a power-of-two scale per 32 channels.
+// 8-bit products of the linear layer with few output tiles.
 //
 // With fewer tiles than the chip has places, a call takes as long as one workgroup's walk through K, and that walk as long as
 // its instructions and waits: 64 x 64 outputs by four waves, K in units of two steps of 128 bytes a row, one barrier per unit.
 // The fragments of a unit are read from LDS while the products of the unit before run, and a unit's loads go out UNITS units
 // ahead.  Row layout, fragments and scale codes as in the large tiles' kernel.
+// K may be split between workgroups; the fp32 partial sums are then added up by a second kernel.
 #include <type_traits>
 
 #include "toma_linear.h"
@@ -28,15 +29,14 @@ __device__ __forceinline__ void buffer_to_lds_run(const uint8_t *base, uint32_t 
 }
 
 // RAGGED: K is no multiple of a step
-template <int KIND, int BM, int BN, int WM, int WN, int UNITS, bool MX_OUT, bool RAGGED>
-__global__ __launch_bounds__(64 * WM * WN) void k_linear_small(const LinArgs a, int tiles_m, int tiles_n) {
+template <int BM, int BN, int WM, int WN, int UNITS, bool MX_OUT, bool RAGGED>
+__global__ __launch_bounds__(64 * WM * WN) void k_linear_small(const LinArgs a, int tiles_m, int tiles_n, int nsplit, float *part) {
   constexpr int NW = WM * WN, WTM = BM / WM, WTN = BN / WN, TM = WTM / 16, TN = WTN / 16;
-  constexpr int ES = KIND == LIN_MX ? 1 : 2, BK = 128 / ES;
+  constexpr int BK = 128;
   constexpr int NIA = BM / 8 / NW, NIB = BN / 8 / NW;  // load instructions (1 KiB) per wave and step
-  constexpr int NS = (BM + BN) / 16, NIS = KIND == LIN_MX ? (NS + 2 * NW - 1) / (2 * NW) : 0;  // per unit: half of four steps' scale codes
+  constexpr int NS = (BM + BN) / 16, NIS = (NS + 2 * NW - 1) / (2 * NW);  // per unit: half of four steps' scale codes
   constexpr int L = 2 * (NIA + NIB) + NIS;             // loads per wave and unit
-  constexpr int PPR = BN / 8;                          // packets per k-row of a k-major stage
-  constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, S_BYTES = KIND == LIN_MX ? (BM + BN) * 16 : 0;
+  constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, S_BYTES = (BM + BN) * 16;
   constexpr int SLOTS = (UNITS + 3) / 2;               // of four steps' codes
   constexpr int B_AT = UNITS * 2 * A_BYTES, S_AT = B_AT + UNITS * 2 * B_BYTES, LDS_BYTES = S_AT + SLOTS * S_BYTES;
   static_assert(TM % 2 == 0 && TM <= 4 && TN <= 4 && (UNITS - 1) * L < 64, "blocks spelled out below; the wait count's range");
@@ -45,35 +45,32 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_small(const LinArgs a, 
 
   int tile_m, tile_n;
   tile_of(blockIdx.x, gridDim.x, tiles_m, tiles_n, tile_m, tile_n);
+  const int split = blockIdx.y;
   const int m0 = tile_m * BM, n0 = tile_n * BN;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), wm = w / WN, wn = w % WN;
   const int g = lane >> 4, c = lane & 15;
-  const int K = a.K, nk = (K + BK - 1) / BK, nu = (nk + 1) >> 1;
+  const int K = a.K, nk_all = (K + BK - 1) / BK;
+  // this workgroup's share of the steps: whole groups of four, whose codes come together
+  const int groups = (nk_all + 3) >> 2;
+  const int u0 = (int)((long long)groups * split / nsplit) * 2, nk = min((int)((long long)groups * (split + 1) / nsplit) * 4, nk_all), nu = (nk + 1) >> 1;
 
   // ---- loads ----------------------------------------------------------------------------------------------------------
-  const uint8_t *xb = static_cast<const uint8_t *>(a.X) + (size_t)m0 * K * ES;
-  const uint8_t *wb = static_cast<const uint8_t *>(a.W) + (KIND == LIN_MX ? (size_t)n0 * K : (size_t)n0 * 2);
-  const size_t w_step = KIND == LIN_MX ? 128 : (size_t)BK * a.N * 2;
+  const uint8_t *xb = static_cast<const uint8_t *>(a.X) + (size_t)m0 * K;
+  const uint8_t *wb = static_cast<const uint8_t *>(a.W) + (size_t)n0 * K;
   // (rows and columns behind the end repeat the last: their results are not stored)
   uint32_t xo[NIA], wo[NIB];
-  int xk[NIA], wk[NIB];  // first channel (k-row) of the lane's packet
+  int xk[NIA], wk[NIB];  // first channel of the lane's packet
 #pragma unroll
   for (int t = 0; t < NIA; t++) {
     const int row = (w * NIA + t) * 8 + (lane >> 3), p = (lane & 7) ^ ((row >> 1) & 7);
-    xk[t] = p * (16 / ES);
-    xo[t] = (uint32_t)min(row, a.rows - 1 - m0) * (uint32_t)(K * ES) + p * 16 + 4096 - 1024 * t;
+    xk[t] = p * 16;
+    xo[t] = (uint32_t)min(row, a.rows - 1 - m0) * (uint32_t)K + p * 16 + 4096 - 1024 * t;
   }
 #pragma unroll
   for (int t = 0; t < NIB; t++) {
-    if constexpr (KIND == LIN_MX) {
-      const int row = (w * NIB + t) * 8 + (lane >> 3), p = (lane & 7) ^ ((row >> 1) & 7);
-      wk[t] = p * 16;
-      wo[t] = (uint32_t)min(row, a.N - 1 - n0) * (uint32_t)K + p * 16 + 4096 - 1024 * t;
-    } else {
-      const int k = (w * NIB + t) * (64 / PPR) + lane / PPR, p = km_place<PPR>(k, lane % PPR);
-      wk[t] = k;
-      wo[t] = (uint32_t)k * (uint32_t)(a.N * 2) + (uint32_t)min(p * 16, (a.N - n0 - 8) * 2) + 4096 - 1024 * t;
-    }
+    const int row = (w * NIB + t) * 8 + (lane >> 3), p = (lane & 7) ^ ((row >> 1) & 7);
+    wk[t] = p * 16;
+    wo[t] = (uint32_t)min(row, a.N - 1 - n0) * (uint32_t)K + p * 16 + 4096 - 1024 * t;
   }
   const uint32_t l0 = lds_addr_of(lds);
   const uint32_t lx = l0 + (uint32_t)(w * NIA * 1024), lw = l0 + B_AT + (uint32_t)(w * NIB * 1024);
@@ -91,7 +88,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_small(const LinArgs a, 
     }
   };
   auto issue = [&](int slot, int u) {
-    if constexpr (KIND == LIN_MX) issue_codes(((u - 1) >> 1) + 1, (u - 1) & 1);  // (a chunk is complete with its first unit's loads)
+    issue_codes(((u - 1) >> 1) + 1, (u - 1) & 1);  // (a chunk is complete with its first unit's loads)
 #pragma unroll
     for (int h = 0; h < 2; h++) {
       const int j = 2 * u + h;
@@ -102,21 +99,17 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_small(const LinArgs a, 
 #pragma unroll
       for (int t = 0; t < NIB; t++) ow[t] = !RAGGED || wk[t] < K - j * BK ? wo[t] : kNoPacket;
       buffer_to_lds_run<NIA>(xb + (size_t)j * 128, bytes, ox, lx + (uint32_t)((2 * slot + h) * A_BYTES));
-      buffer_to_lds_run<NIB>(wb + (size_t)j * w_step, bytes, ow, lw + (uint32_t)((2 * slot + h) * B_BYTES));
+      buffer_to_lds_run<NIB>(wb + (size_t)j * 128, bytes, ow, lw + (uint32_t)((2 * slot + h) * B_BYTES));
     }
   };
 
   // ---- fragments ------------------------------------------------------------------------------------------------------
   const uint32_t p0 = (uint32_t)(g ^ ((c >> 1) & 7)) << 4;
-  const int kq = 8 * g + (c >> 2), kcol = wn * WTN + 4 * (c & 3);  // (k-major weights: transpose reads)
-  constexpr int NRW = KIND == LIN_MX ? 2 : TN;
-  lds_ptr rx[2], rw[NRW];
+  lds_ptr rx[2], rw[2];
 #pragma unroll
-  for (int e = 0; e < 2; e++) rx[e] = (lds_ptr)(lds + (wm * WTM + c) * 128 + (p0 ^ (64u * e)));
-#pragma unroll
-  for (int e = 0; e < NRW; e++) {
-    if constexpr (KIND == LIN_MX) rw[e] = (lds_ptr)(lds + B_AT + (wn * WTN + c) * 128 + (p0 ^ (64u * e)));
-    else rw[e] = (lds_ptr)(lds + B_AT + (kq * PPR + km_place<PPR>(kq, (kcol + 16 * e) >> 3)) * 16 + (kcol & 7) * 2);
+  for (int e = 0; e < 2; e++) {
+    rx[e] = (lds_ptr)(lds + (wm * WTM + c) * 128 + (p0 ^ (64u * e)));
+    rw[e] = (lds_ptr)(lds + B_AT + (wn * WTN + c) * 128 + (p0 ^ (64u * e)));
   }
   const lds_ptr rs = (lds_ptr)(lds + S_AT + c * 16);
   i32x8 fx[2][2][TM], fw[2][2][TN];  // [set][half of the unit]
@@ -131,29 +124,15 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_small(const LinArgs a, 
       for (int i = 0; i < TM; i++)
         fx[set][h][i] = join_halves(*(lds_u32x4_ptr)(rx[0] + ax + h * A_BYTES + i * 2048), *(lds_u32x4_ptr)(rx[1] + ax + h * A_BYTES + i * 2048));
 #pragma unroll
-      for (int j = 0; j < TN; j++) {
-        if constexpr (KIND == LIN_MX) {
-          fw[set][h][j] = join_halves(*(lds_u32x4_ptr)(rw[0] + aw + h * B_BYTES + j * 2048), *(lds_u32x4_ptr)(rw[1] + aw + h * B_BYTES + j * 2048));
-        } else {
-          u32x4 f[2];
-#pragma unroll
-          for (int e = 0; e < 2; e++) {
-            const lds_ptr at = rw[j] + aw + h * B_BYTES + 32 * e * PPR * 16;
-            const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)at));
-            const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(at + 4 * PPR * 16)));
-            f[e] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3);
-          }
-          fw[set][h][j] = join_halves(f[0], f[1]);
-        }
-      }
+      for (int j = 0; j < TN; j++)
+        fw[set][h][j] = join_halves(*(lds_u32x4_ptr)(rw[0] + aw + h * B_BYTES + j * 2048), *(lds_u32x4_ptr)(rw[1] + aw + h * B_BYTES + j * 2048));
     }
-    if constexpr (KIND == LIN_MX) {  // a row's codes of the unit's two steps: eight bytes
-      const lds_ptr at = rs + ((u >> 1) % SLOTS * S_BYTES + (u & 1) * 8);
+    // a row's codes of the unit's two steps: eight bytes
+    const lds_ptr at = rs + ((u >> 1) % SLOTS * S_BYTES + (u & 1) * 8);
 #pragma unroll
-      for (int i = 0; i < TM; i++) raw_x[i] = *(lds_u32x2_ptr)(at + (wm * WTM + 16 * i) * 16);
+    for (int i = 0; i < TM; i++) raw_x[i] = *(lds_u32x2_ptr)(at + (wm * WTM + 16 * i) * 16);
 #pragma unroll
-      for (int j = 0; j < TN; j++) raw_w[j] = *(lds_u32x2_ptr)(at + (BM + wn * WTN + 16 * j) * 16);
-    }
+    for (int j = 0; j < TN; j++) raw_w[j] = *(lds_u32x2_ptr)(at + (BM + wn * WTN + 16 * j) * 16);
   };
   const uint32_t tail_mask = K % 128 ? 0xffffffffu >> (32 - (K >> 5) % 4 * 8) : 0u;  // codes of the last group that stand for channels
   auto gather_codes = [&](int u) {
@@ -181,13 +160,13 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_small(const LinArgs a, 
   using std::integral_constant;
   constexpr integral_constant<int, 0> even{};
   constexpr integral_constant<int, 1> odd{};
-  if constexpr (KIND == LIN_MX) issue_codes(0, 0);
+  issue_codes(u0 >> 1, 0);
 #pragma unroll
-  for (int u = 0; u < UNITS; u++) issue(u, u);
+  for (int u = 0; u < UNITS; u++) issue(u, u0 + u);
   wait_vmcnt<(UNITS - 1) * L>();
   meet();
-  read(even, 0, 0);
-  if constexpr (KIND == LIN_MX) gather_codes(0);
+  read(even, 0, u0);
+  gather_codes(u0);
   __builtin_amdgcn_s_waitcnt(0xc07f);
   wait_vmcnt<(UNITS - 2) * L>();
   meet();
@@ -199,36 +178,29 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_small(const LinArgs a, 
     read(integral_constant<int, set ^ 1>(), next, u + 1);
     issue(slot, u + UNITS);
     __builtin_amdgcn_sched_barrier(0);
-    auto row = [&](auto h_, auto i_, int e) {
+    auto row = [&](auto h_, auto i_) {
       constexpr int h = decltype(h_)::value, i = decltype(i_)::value;
       auto one = [&](auto j_) {
         constexpr int j = decltype(j_)::value;
-        if constexpr (i < TM && j < TN) {
-          if constexpr (KIND == LIN_MX)
-            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[set][h][j], fx[set][h][i], acc[i][j], 0, 0, j, (int)cw[h], i, (int)cx[h]);
-          else
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_half(fw[set][h][j], e), bf16_half(fx[set][h][i], e), acc[i][j], 0, 0, 0);
-        }
+        if constexpr (i < TM && j < TN)
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[set][h][j], fx[set][h][i], acc[i][j], 0, 0, j, (int)cw[h], i, (int)cx[h]);
       };
       one(integral_constant<int, 0>()); one(integral_constant<int, 1>()); one(integral_constant<int, 2>()); one(integral_constant<int, 3>());
     };
     auto half = [&](auto h_) {
-#pragma unroll
-      for (int e = 0; e < (KIND == LIN_MX ? 1 : 2); e++) {
-        row(h_, integral_constant<int, 0>(), e); row(h_, integral_constant<int, 1>(), e);
-        row(h_, integral_constant<int, 2>(), e); row(h_, integral_constant<int, 3>(), e);
-      }
+      row(h_, integral_constant<int, 0>()); row(h_, integral_constant<int, 1>());
+      row(h_, integral_constant<int, 2>()); row(h_, integral_constant<int, 3>());
     };
     half(even);
     half(odd);
     __builtin_amdgcn_sched_barrier(0);
-    if constexpr (KIND == LIN_MX) gather_codes(u + 1);
+    gather_codes(u + 1);
     __builtin_amdgcn_s_waitcnt(0xc07f);
     wait_vmcnt<(UNITS - 2) * L>();
     meet();
     slot = next;
   };
-  for (int u = 0;;) {
+  for (int u = u0;;) {
     unit(even, u);
     if (++u >= nu) break;
     unit(odd, u);
@@ -236,34 +208,74 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_small(const LinArgs a, 
   }
   wait_vmcnt<0>();  // (the zeros of the units behind the last)
   meet();
+  if (part) {  // fp32 partial sums [split][rows][N]; k_linear_finish adds them up
+#pragma unroll
+    for (int i = 0; i < TM; i++) {
+      const int m = m0 + wm * WTM + 16 * i + c;
+#pragma unroll
+      for (int j = 0; j < TN; j++) {
+        const int n = n0 + wn * WTN + 16 * j + 4 * g;
+        if (m < a.rows && n < a.N) *reinterpret_cast<f32x4 *>(part + ((size_t)split * a.rows + m) * a.N + n) = acc[i][j];
+      }
+    }
+    return;
+  }
   linear_epilogue<TM, TN, MX_OUT>(a, acc, reinterpret_cast<float *>(lds) + w * kEpilogueFloats<TN>, m0 + wm * WTM, n0 + wn * WTN, lane);
 }
 
-template <int KIND, int BM, int BN, int WM, int WN, int UNITS>
-static void go(const LinArgs &a, bool mx_out, hipStream_t st) {
-  const int tm = (a.rows + BM - 1) / BM, tn = (a.N + BN - 1) / BN;
-  const dim3 grid((unsigned)(tm * (long long)tn)), block(64 * WM * WN);
-  const bool ragged = a.K % (KIND == LIN_MX ? 128 : 64) != 0;
-  auto run = [&](auto out) {
-    constexpr bool o = decltype(out)::value;
-    if (ragged) hipLaunchKernelGGL((k_linear_small<KIND, BM, BN, WM, WN, UNITS, o, true>), grid, block, 0, st, a, tm, tn);
-    else hipLaunchKernelGGL((k_linear_small<KIND, BM, BN, WM, WN, UNITS, o, false>), grid, block, 0, st, a, tm, tn);
-  };
-  if constexpr (KIND == LIN_MX) {
-    if (mx_out) return run(std::true_type());
+// Sum of the partial products in the order of K, then the epilogue.  One thread per eight columns; a row's threads cover whole
+// groups of 128 columns, so that a quad is one packed block and the padding's codes have their writer.
+template <bool MX_OUT>
+__global__ __launch_bounds__(256) void k_linear_finish(const LinArgs a, int nsplit, const float *__restrict__ part, int per_row) {
+  const size_t t = (size_t)blockIdx.x * 256 + threadIdx.x;
+  const int m = (int)(t / per_row), n = (int)(t - (size_t)m * per_row) * 8;
+  const bool in = m < a.rows && n < a.N;
+  const size_t at = (size_t)m * a.N + n;
+  F8 v;
+#pragma unroll
+  for (int i = 0; i < 8; i++) v.v[i] = 0.0f;
+  if (in) {
+    for (int s = 0; s < nsplit; s++) {
+      const F8 p = load8(part + (size_t)s * a.rows * a.N + at);
+#pragma unroll
+      for (int i = 0; i < 8; i++) v.v[i] += p.v[i];
+    }
+    if (a.bias) add8(v, pkt_load(static_cast<const bf16_t *>(a.bias) + n));
+    activate<false>(v.v, a.act);
+    if (a.R) add8(v, pkt_load(static_cast<const bf16_t *>(a.R) + at));
+    if (a.R2) add8(v, pkt_load(static_cast<const bf16_t *>(a.R2) + at));
   }
-  run(std::false_type());
+  if constexpr (MX_OUT) {
+    u32x2 o;
+    const uint32_t code = mx_pack_quad(v, o);
+    if (in) *reinterpret_cast<u32x2 *>(static_cast<uint8_t *>(a.Y) + at) = o;
+    if (m < a.rows && (n & 31) == 0 && (n >> 5) < a.ys_stride) a.Ys[(size_t)m * a.ys_stride + (n >> 5)] = in ? (uint8_t)code : 0;
+  } else if (in) {
+    store8(static_cast<bf16_t *>(a.Y) + at, v);
+  }
 }
 
-int launch_linear_small(int kind, int which, int, const LinArgs &a, bool mx_out, hipStream_t st) {
-#define TILES(KIND) \
-  if (which == 2) go<KIND, 64, 64, 2, 2, 2>(a, mx_out, st); \
-  else if (which == 3) go<KIND, 64, 64, 2, 2, 4>(a, mx_out, st); \
-  else if (which == 4) go<KIND, 64, 128, 2, 2, 2>(a, mx_out, st); \
-  else if (which == 5) go<KIND, 64, 128, 2, 2, 3>(a, mx_out, st); \
-  else go<KIND, 128, 128, 2, 2, 2>(a, mx_out, st);
-  if (kind == LIN_MX) { TILES(LIN_MX) } else { TILES(LIN_BF16) }
-  return launch_status();
+template <int BM, int BN, int WM, int WN, int UNITS>
+static void go(const LinArgs &a, bool mx_out, int nsplit, float *part, hipStream_t st) {
+  const int tm = (a.rows + BM - 1) / BM, tn = (a.N + BN - 1) / BN;
+  const dim3 grid((unsigned)(tm * (long long)tn), (unsigned)nsplit), block(64 * WM * WN);
+  auto run = [&](auto out, auto ragged) {
+    hipLaunchKernelGGL((k_linear_small<BM, BN, WM, WN, UNITS, decltype(out)::value, decltype(ragged)::value>), grid, block, 0, st, a, tm, tn, nsplit,
+                       nsplit > 1 ? part : nullptr);
+  };
+  const bool ragged = a.K % 128 != 0;
+  if (mx_out && nsplit == 1) ragged ? run(std::true_type(), std::true_type()) : run(std::true_type(), std::false_type());
+  else ragged ? run(std::false_type(), std::true_type()) : run(std::false_type(), std::false_type());
+  if (nsplit > 1) {
+    const int per_row = mx_out ? a.ys_stride * 4 : a.N / 8;
+    const dim3 blocks((unsigned)(((size_t)a.rows * per_row + 255) / 256));
+    if (mx_out) hipLaunchKernelGGL(k_linear_finish<true>, blocks, dim3(256), 0, st, a, nsplit, part, per_row);
+    else hipLaunchKernelGGL(k_linear_finish<false>, blocks, dim3(256), 0, st, a, nsplit, part, per_row);
+  }
+}
+
+void launch_linear_small(const LinArgs &a, bool mx_out, int nsplit, float *part, hipStream_t st) {
+  go<64, 64, 2, 2, 2>(a, mx_out, nsplit, part, st);
 }
 
 }  // namespace toma

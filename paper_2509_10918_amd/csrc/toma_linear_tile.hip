@@ -6,8 +6,6 @@
 // bf16: whole cache lines), through two stages in LDS that the load-to-LDS path fills.
 // A 128-byte row of a stage is eight 16-byte packets; packet p of row r lies at place p ^ (r >> 1 & 7), which spreads the 16 rows
 // that a fragment read takes over all banks.
-#include <stdlib.h>
-
 #include "toma_linear.h"
 
 namespace toma {
@@ -295,15 +293,9 @@ static void go(const LinArgs &a, bool mx_out, hipStream_t st) {
   hipLaunchKernelGGL((k_linear_tile<KIND, BM, BN, WM, WN, false>), grid, block, 0, st, a, tm, tn);
 }
 
-int launch_linear_tile(int kind, const LinArgs &a, bool mx_out, hipStream_t st) {
-  KernelTimer kt(K_LINEAR, st);
-  const int which = getenv("LIN_TILE") ? atoi(getenv("LIN_TILE")) : 0;
-  if (which >= 2) return launch_linear_small(kind, which, 0, a, mx_out, st);
-#define TILES(KIND) \
-  if (which == 0) go<KIND, 256, 256, 2, 4>(a, mx_out, st); \
-  else go<KIND, 128, 128, 2, 2>(a, mx_out, st);
-  if (kind == LIN_MX) { TILES(LIN_MX) } else { TILES(LIN_BF16) }
-  return launch_status();
+void launch_linear_tile(int kind, bool large, const LinArgs &a, bool mx_out, hipStream_t st) {
+  if (kind == LIN_MX) large ? go<LIN_MX, 256, 256, 2, 4>(a, mx_out, st) : go<LIN_MX, 128, 128, 2, 2>(a, mx_out, st);
+  else large ? go<LIN_BF16, 256, 256, 2, 4>(a, mx_out, st) : go<LIN_BF16, 128, 128, 2, 2>(a, mx_out, st);
 }
 
 }  // namespace toma
