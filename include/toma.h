@@ -389,6 +389,9 @@ int toma_profile_read(const char *kernel, int32_t *launches, float *total_ms);
  * products actually executed.  Host arithmetic only; TOMA_ERR_UNSUPPORTED when the product does not
  * take the tiled path. */
 int toma_profile_map_product(const toma_desc *desc, int which, int32_t *out3);
+/* Tile and K split that toma_linear takes for this descriptor: out3 = {rows per workgroup, columns, K split}.  Host arithmetic
+ * only. */
+int toma_profile_linear(const toma_linear_desc *desc, int32_t *out3);
 /* toma_select (Sec. 4.1, Alg. 2) with the greedy kernel replaced by a variant of itself that also
  * adds up, per wave, the shader clocks spent in each part of a round - a measurement aid for the one
  * kernel whose time is a chain of dependent steps rather than bytes or products.  idx as toma_select.

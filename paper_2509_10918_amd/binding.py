@@ -21,7 +21,8 @@ EXPORTS = ("toma_workspace_bytes", "toma_status_string", "toma_select", "toma_se
            "toma_unmerge_recompute", "toma_layer", "toma_mlp", "toma_mx_scale_stride", "toma_mx_quantize", "toma_mx_quantize_weight",
            "toma_mx_dequantize", "toma_rmsnorm", "toma_linear_workspace_bytes", "toma_linear", "toma_ffn_workspace_bytes", "toma_ffn",
            "toma_profile_enable",
-           "toma_profile_kernel_name", "toma_profile_read", "toma_profile_map_product", "toma_profile_greedy_parts")
+           "toma_profile_kernel_name", "toma_profile_read", "toma_profile_map_product", "toma_profile_linear",
+           "toma_profile_greedy_parts")
 
 
 class TomaError(RuntimeError):
@@ -115,7 +116,8 @@ def lib():
         L.toma_linear_workspace_bytes.argtypes = L.toma_ffn_workspace_bytes.argtypes = [vp]
         L.toma_linear.argtypes = [vp] * 10 + [sz, vp]
         L.toma_ffn.argtypes = [vp] * 12 + [sz, vp]
-        for name in ("toma_mx_quantize", "toma_mx_quantize_weight", "toma_mx_dequantize", "toma_rmsnorm", "toma_linear", "toma_ffn"):
+        L.toma_profile_linear.argtypes = [vp, ctypes.POINTER(ctypes.c_int32)]
+        for name in ("toma_profile_linear", "toma_mx_quantize", "toma_mx_quantize_weight", "toma_mx_dequantize", "toma_rmsnorm", "toma_linear", "toma_ffn"):
             getattr(L, name).restype = ctypes.c_int
         for name in ("toma_select", "toma_merge", "toma_map_build", "toma_merge_cached", "toma_attend", "toma_cross_attend", "toma_unmerge", "toma_unmerge_pinv", "toma_recompute_cache_bytes", "toma_merge_recompute",
            "toma_unmerge_recompute",
@@ -431,6 +433,13 @@ def toma_profile_map_product(desc, which):
     out = (ctypes.c_int32 * 3)()
     rc = lib().toma_profile_map_product(_ref(desc), int(which), out)
     return None if rc != 0 else tuple(out)
+
+
+def toma_profile_linear(desc):
+    """(rows, columns, K split) of toma_linear's workgroups for this descriptor."""
+    out = (ctypes.c_int32 * 3)()
+    _check(lib().toma_profile_linear(_ref(desc), out), "toma_profile_linear")
+    return tuple(out)
 
 
 def toma_profile_greedy_parts(desc, X, idx, parts, ws):

@@ -527,6 +527,14 @@ TOMA_API int toma_linear(const toma_linear_desc *desc, const void *X, const void
   return launch_linear(*desc, X, Xs_opt, W, Ws_opt, bias_opt, R_opt, nullptr, Y, Ys_opt, ws, static_cast<hipStream_t>(stream));
 }
 
+TOMA_API int toma_profile_linear(const toma_linear_desc *desc, int32_t *out3) {
+  const int rc = check_linear(desc);
+  if (rc != TOMA_OK) return rc;
+  if (!out3) return TOMA_ERR_NULL;
+  plan_linear_tile(*desc, out3);
+  return TOMA_OK;
+}
+
 // The stages of a feed-forward block and where their outputs lie in the workspace.
 struct FfnPlan {
   toma_norm_desc norm;

@@ -257,6 +257,7 @@ int launch_mx_dequantize(int y_type, int rows, int K, const void *Q, const void 
 int launch_rmsnorm(const toma_norm_desc &d, const void *X, const void *R, const void *gamma, void *H, void *Y, void *Ys,
                    hipStream_t st);
 size_t linear_workspace_bytes(const toma_linear_desc &d);
+void plan_linear_tile(const toma_linear_desc &d, int32_t *out3);  // tile and K split
 // R2: a second residual (the feed-forward block's stream is X + R in its last epilogue)
 int launch_linear(const toma_linear_desc &d, const void *X, const void *Xs, const void *W, const void *Ws, const void *bias,
                   const void *R, const void *R2, void *Y, void *Ys, void *ws, hipStream_t st);

@@ -1,5 +1,4 @@
 // Linear layer with its epilogue, Y = act(X W + bias) + R: which kernel a shape takes, and the fp32 and small bf16 products.
-#include <stdlib.h>
 #include <algorithm>
 
 #include "toma_linear.h"
@@ -54,26 +53,81 @@ template <typename T> struct EpiPol {
 // the planner's and the load-to-LDS path's smallest row count (rows past the end are clamped, so fewer do as well)
 static int gemm_rows(int rows) { return std::max(rows, 8); }
 
+// ---- which kernel --------------------------------------------------------------------------------------------------------
+// Estimated times in microseconds, fitted to measurements of every kernel on the same shapes (replayed graphs, so without host
+// time).  A kernel's workgroups run in rounds of what the chip holds; a round costs a fixed part (first loads, epilogue) and a part
+// per K step of 128 bytes a row, which is smaller where CUs are left over or hold one workgroup instead of two.
+// Measured and estimated, us (bf16, rows x K x N):            large        medium       planned tiles
+//   16384 x 4096 x 8192                                       790 / 778    1000 / 970   1088
+//   4096 x 640 x 2560                                         21.9 / 21.0  23.1 / 26.3  27.9 / 23.4
+//   1024 x 1280 x 5120                                        30.4 / 30.0  22.3 / 24.0  23.9 / 22.0
+//   1024 x 5120 x 1280                                        84 / 93      49 / 53      25.3 / 29.2
+// and in 8 bits:                                              large        medium       small
+//   16384 x 4096 x 8192                                       521 / 513    625 / 660    -
+//   1024 x 1280 x 5120                                        23.2 / 22.0  16.5 / 16.0  20.4 / 15.2
+//   1024 x 5120 x 1280                                        59 / 61      31 / 31      21.5 / 20.9
+//   77 x 8192 x 1280                                          87 / 92      43 / 45      20.7 / 21.8, K split in 5: 11.3 / 11.2
+struct RoundCost { int tile, slots; double fixed, full, few; };  // few: per step where at most half of the slots are taken
+constexpr RoundCost kLarge[2] = {{256, 256, 7.0, 1.4, 1.05}, {256, 256, 7.0, 1.78, 1.3}};  // bf16, 8 bits
+constexpr RoundCost kMedium[2] = {{128, 512, 5.0, 0.85, 0.58}, {128, 512, 5.0, 0.9, 0.6}};
+constexpr RoundCost kSmall = {64, 512, 2.5, 0.41, 0.27};                                     // 8 bits
+
+static double rounds_cost(const RoundCost &c, int rows, int N, int steps, int nsplit = 1) {
+  const long long wgs = (long long)((rows + c.tile - 1) / c.tile) * ((N + c.tile - 1) / c.tile) * nsplit;
+  const long long rest = wgs % c.slots;
+  double t = 2.0 + (double)(wgs / c.slots) * (c.fixed + c.full * steps);
+  if (rest) t += c.fixed + (2 * rest > c.slots ? c.full : c.few) * steps;
+  return t;
+}
+
+// The fp32 partial sums of a K split are written and read once, by a kernel more.
+static double split_cost(int rows, int N, int nsplit) { return 3.0 + (8.0 * nsplit + 4.0) * rows * N / 4.0e6; }
+
 enum Path { PATH_LARGE, PATH_MEDIUM, PATH_SMALL };
-struct LinPlan { Path path; int nsplit; };
+struct LinPlan { Path path; int bm, bn, nsplit; };
 
 static LinPlan plan_linear(const toma_linear_desc &d) {
-  const char *e = getenv("LIN_TILE");
-  const int es = d.x_type == TOMA_F32 ? 4 : 2;
-  if (e && d.x_type != TOMA_F32) {
-    const int t = atoi(e);
-    if (t == 0) return {PATH_LARGE, 1};
-    if (t == 1) return {PATH_MEDIUM, 1};
-    if (d.x_type == TOMA_MX8) return {PATH_SMALL, std::max(1, std::min(t - 1, (d.K + 511) / 512))};
-    return {PATH_SMALL, gemm_async_fits(gemm_rows(d.rows), d.N, d.K, es) ? plan_gemm_async(gemm_rows(d.rows), d.N, d.K, 1, es, true, false, true, 1).nsplit : 1};
+  if (d.x_type == TOMA_MX8) {
+    const int steps = (d.K + 127) / 128, groups = (steps + 3) / 4;
+    LinPlan best{PATH_LARGE, 256, 256, 1};
+    double least = rounds_cost(kLarge[1], d.rows, d.N, steps);
+    auto offer = [&](double t, const LinPlan &p) {
+      if (t < least) { least = t; best = p; }
+    };
+    offer(rounds_cost(kMedium[1], d.rows, d.N, steps), {PATH_MEDIUM, 128, 128, 1});
+    offer(rounds_cost(kSmall, d.rows, d.N, steps), {PATH_SMALL, 64, 64, 1});
+    for (int ns = 2; ns <= 8 && ns <= groups; ns++)
+      offer(rounds_cost(kSmall, d.rows, d.N, (groups + ns - 1) / ns * 4, ns) + split_cost(d.rows, d.N, ns), {PATH_SMALL, 64, 64, ns});
+    return best;
   }
-  int nsplit = 1;
-  if (d.x_type != TOMA_MX8 && gemm_async_fits(gemm_rows(d.rows), d.N, d.K, es)) nsplit = plan_gemm_async(gemm_rows(d.rows), d.N, d.K, 1, es, true, false, true, 1).nsplit;
-  return {PATH_SMALL, nsplit};
+  const int es = d.x_type == TOMA_F32 ? 4 : 2, rows = gemm_rows(d.rows);
+  LinPlan best{PATH_SMALL, 64, 64, 1};
+  double least;
+  if (gemm_async_fits(rows, d.N, d.K, es)) {
+    const GemmPlan p = plan_gemm_async(rows, d.N, d.K, 1, es, true, false, true, 1);
+    best = {PATH_SMALL, p.bm, p.bn, p.nsplit};
+    least = p.cost / 2100.0;
+  } else {  // the register-staged kernel: 64 x 64 tiles, one per CU at a time
+    const GemmShape g = choose_gemm_shape(rows, d.N, 1);
+    best = {PATH_SMALL, g.bm, g.bn, 1};
+    const long long wgs = (long long)((rows + 63) / 64) * ((d.N + 63) / 64);
+    least = 2.5 + (double)((wgs + 255) / 256) * 0.4 * ((d.K + 63) / 64);
+  }
+  if (d.x_type == TOMA_BF16) {
+    const int steps = (d.K + 63) / 64;
+    const double large = rounds_cost(kLarge[0], d.rows, d.N, steps), medium = rounds_cost(kMedium[0], d.rows, d.N, steps);
+    if (std::min(large, medium) < least) best = large < medium ? LinPlan{PATH_LARGE, 256, 256, 1} : LinPlan{PATH_MEDIUM, 128, 128, 1};
+  }
+  return best;
+}
+
+void plan_linear_tile(const toma_linear_desc &d, int32_t *out3) {
+  const LinPlan p = plan_linear(d);
+  out3[0] = p.bm; out3[1] = p.bn; out3[2] = p.nsplit;
 }
 
 template <typename T>
-static void linear_typed(const LinArgs &a, const LinPlan &plan, float *part, hipStream_t st) {
+static void linear_typed(const LinArgs &a, float *part, hipStream_t st) {
   EpiPol<T> p{};
   p.In = static_cast<const T *>(a.X); p.Wt = static_cast<const T *>(a.W); p.bias = static_cast<const T *>(a.bias);
   p.R = static_cast<const T *>(a.R); p.R2 = static_cast<const T *>(a.R2); p.Out = static_cast<T *>(a.Y);
@@ -101,9 +155,9 @@ int launch_linear(const toma_linear_desc &d, const void *X, const void *Xs, cons
     KernelTimer kt(K_LINEAR, st);
     launch_linear_small(a, mx_out, plan.nsplit, part, st);
   } else if (d.x_type == TOMA_BF16) {
-    linear_typed<bf16_t>(a, plan, part, st);
+    linear_typed<bf16_t>(a, part, st);
   } else {
-    linear_typed<float>(a, plan, part, st);
+    linear_typed<float>(a, part, st);
   }
   return launch_status();
 }

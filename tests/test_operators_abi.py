@@ -96,6 +96,24 @@ def test_linear_refusals():
             assert f(_p(d), X, c, X, c, None, None, X, None, X, 128, None) == 4
 
 
+def test_linear_tile_is_host_arithmetic():
+    """Tile and K split come from the descriptor alone; the scratch is what the split's partial sums take."""
+    L = tb.lib()
+    seen = set()
+    for x_type, y_type in (("bf16", None), ("mx8", "bf16"), ("f32", None)):
+        for rows, K, N in ((16384, 4096, 8192), (1025, 1376, 4104), (512, 640, 640), (77, 8192, 1280), (1, 8192, 640)):
+            d = tb.make_linear_desc(rows, K, N, x_type, y_type)
+            bm, bn, split = tb.toma_profile_linear(d)
+            assert bm in (64, 128, 256) and bn in (64, 128, 256) and 1 <= split <= 8
+            need = tb.toma_linear_workspace_bytes(d)
+            assert need == 0 if split == 1 else need >= 4 * split * rows * N
+            seen.add((x_type, bm, bn, split > 1))
+    assert {("bf16", 256, 256, False), ("mx8", 256, 256, False), ("mx8", 128, 128, False), ("mx8", 64, 64, False), ("mx8", 64, 64, True),
+            ("bf16", 64, 64, True)} <= seen
+    d = tb.make_linear_desc(16, 64, 64, "bf16")
+    assert L.toma_profile_linear(_p(d), None) == 1 and L.toma_profile_linear(None, None) == 1
+
+
 def test_ffn_refusals():
     L = tb.lib()
     d = tb.make_ffn_desc(100, 64, 256, 1e-6, "bf16", "mx8")
