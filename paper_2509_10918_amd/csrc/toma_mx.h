@@ -75,12 +75,21 @@ __device__ __forceinline__ void store8(float *p, const F8 &x) {
   *reinterpret_cast<f32x4 *>(p) = a;
   *reinterpret_cast<f32x4 *>(p + 4) = b;
 }
+// Largest finite magnitude of eight values.  The maximum drops NaN by itself; infinities are looked for only where the result is one.
+__device__ __forceinline__ float mx_largest(const F8 &x) {
+  float m = fmaxf(__builtin_fabsf(x.v[0]), __builtin_fabsf(x.v[1]));
+#pragma unroll
+  for (int i = 2; i < 8; i += 2) m = fmaxf(fmaxf(m, __builtin_fabsf(x.v[i])), __builtin_fabsf(x.v[i + 1]));  // (one max3 each)
+  if (__builtin_expect(!(m < __builtin_inff()), 0)) {
+    m = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; i++) m = fmaxf(m, mx_magnitude(x.v[i]));
+  }
+  return m;
+}
 // Packs a block whose 32 channels four consecutive lanes of a quad hold, eight each.  Returns the code; q: the lane's eight bytes.
 __device__ __forceinline__ uint32_t mx_pack_quad(const F8 &x, u32x2 &q) {
-  float m = 0.0f;
-#pragma unroll
-  for (int i = 0; i < 8; i++) m = fmaxf(m, mx_magnitude(x.v[i]));
-  const uint32_t code = mx_code(quad_max_f32(m));
+  const uint32_t code = mx_code(quad_max_f32(mx_largest(x)));
   const float inv = mx_inverse(code);
   q[0] = mx_pack4(x.v[0], x.v[1], x.v[2], x.v[3], inv);
   q[1] = mx_pack4(x.v[4], x.v[5], x.v[6], x.v[7], inv);
