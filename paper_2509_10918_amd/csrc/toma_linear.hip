@@ -67,16 +67,20 @@ static int gemm_rows(int rows) { return std::max(rows, 8); }
 //   1024 x 1280 x 5120                                        23.2 / 22.0  16.5 / 16.0  20.4 / 15.2
 //   1024 x 5120 x 1280                                        59 / 61      31 / 31      21.5 / 20.9
 //   77 x 8192 x 1280                                          87 / 92      43 / 45      20.7 / 21.8, K split in 5: 11.3 / 11.2
-struct RoundCost { int tile, slots; double fixed, full, few; };  // few: per step where at most half of the slots are taken
-constexpr RoundCost kLarge[2] = {{256, 256, 7.0, 1.4, 1.05}, {256, 256, 7.0, 1.78, 1.3}};  // bf16, 8 bits
-constexpr RoundCost kMedium[2] = {{128, 512, 5.0, 0.85, 0.58}, {128, 512, 5.0, 0.9, 0.6}};
-constexpr RoundCost kSmall = {64, 512, 2.5, 0.41, 0.27};                                     // 8 bits
+// few: per step where at most half of the slots are taken; act: per round for each activation (two workgroups on a CU run one's
+// epilogue beside the other's products: 16384 x 640 x 2560 in 8 bits 53 and 48 us without activation, 69 and 58 with gelu)
+struct RoundCost { int tile, slots; double fixed, full, few, act[4]; };
+constexpr RoundCost kLarge[2] = {{256, 256, 7.0, 1.4, 1.05, {0.0, 5.3, 3.0, 1.0}},     // bf16
+                                 {256, 256, 7.0, 1.78, 1.3, {0.0, 5.3, 3.0, 1.0}}};    // 8 bits
+constexpr RoundCost kMedium[2] = {{128, 512, 5.0, 0.85, 0.58, {0.0, 1.9, 1.2, 0.4}}, {128, 512, 5.0, 0.9, 0.6, {0.0, 1.9, 1.2, 0.4}}};
+constexpr RoundCost kSmall = {64, 512, 2.5, 0.41, 0.27, {0.0, 0.6, 0.4, 0.2}};         // 8 bits
 
-static double rounds_cost(const RoundCost &c, int rows, int N, int steps, int nsplit = 1) {
-  const long long wgs = (long long)((rows + c.tile - 1) / c.tile) * ((N + c.tile - 1) / c.tile) * nsplit;
+static double rounds_cost(const RoundCost &c, const toma_linear_desc &d, int steps, int nsplit = 1) {
+  const long long wgs = (long long)((d.rows + c.tile - 1) / c.tile) * ((d.N + c.tile - 1) / c.tile) * nsplit;
   const long long rest = wgs % c.slots;
-  double t = 2.0 + (double)(wgs / c.slots) * (c.fixed + c.full * steps);
-  if (rest) t += c.fixed + (2 * rest > c.slots ? c.full : c.few) * steps;
+  const double fixed = c.fixed + (nsplit == 1 ? c.act[d.act] : 0.0);
+  double t = 2.0 + (double)(wgs / c.slots) * (fixed + c.full * steps);
+  if (rest) t += fixed + (2 * rest > c.slots ? c.full : c.few) * steps;
   return t;
 }
 
@@ -90,14 +94,14 @@ static LinPlan plan_linear(const toma_linear_desc &d) {
   if (d.x_type == TOMA_MX8) {
     const int steps = (d.K + 127) / 128, groups = (steps + 3) / 4;
     LinPlan best{PATH_LARGE, 256, 256, 1};
-    double least = rounds_cost(kLarge[1], d.rows, d.N, steps);
+    double least = rounds_cost(kLarge[1], d, steps);
     auto offer = [&](double t, const LinPlan &p) {
       if (t < least) { least = t; best = p; }
     };
-    offer(rounds_cost(kMedium[1], d.rows, d.N, steps), {PATH_MEDIUM, 128, 128, 1});
-    offer(rounds_cost(kSmall, d.rows, d.N, steps), {PATH_SMALL, 64, 64, 1});
+    offer(rounds_cost(kMedium[1], d, steps), {PATH_MEDIUM, 128, 128, 1});
+    offer(rounds_cost(kSmall, d, steps), {PATH_SMALL, 64, 64, 1});
     for (int ns = 2; ns <= 8 && ns <= groups; ns++)
-      offer(rounds_cost(kSmall, d.rows, d.N, (groups + ns - 1) / ns * 4, ns) + split_cost(d.rows, d.N, ns), {PATH_SMALL, 64, 64, ns});
+      offer(rounds_cost(kSmall, d, (groups + ns - 1) / ns * 4, ns) + split_cost(d.rows, d.N, ns), {PATH_SMALL, 64, 64, ns});
     return best;
   }
   const int es = d.x_type == TOMA_F32 ? 4 : 2, rows = gemm_rows(d.rows);
@@ -115,7 +119,7 @@ static LinPlan plan_linear(const toma_linear_desc &d) {
   }
   if (d.x_type == TOMA_BF16) {
     const int steps = (d.K + 63) / 64;
-    const double large = rounds_cost(kLarge[0], d.rows, d.N, steps), medium = rounds_cost(kMedium[0], d.rows, d.N, steps);
+    const double large = rounds_cost(kLarge[0], d, steps), medium = rounds_cost(kMedium[0], d, steps);
     if (std::min(large, medium) < least) best = large < medium ? LinPlan{PATH_LARGE, 256, 256, 1} : LinPlan{PATH_MEDIUM, 128, 128, 1};
   }
   return best;

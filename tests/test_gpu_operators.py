@@ -279,7 +279,7 @@ def test_linear_of_many_rows(x_type, rows, K, N):
 TILES = [("bf16", 4096, 640, 2560, (256, 256, 1)), ("bf16", 4097, 648, 2568, (256, 256, 1)), ("bf16", 3900, 72, 2888, (128, 128, 1)),
          ("bf16", 1024, 1280, 5120, None), ("bf16", 2000, 1288, 2000, (128, 128, 1)), ("bf16", 1025, 1344, 4104, None), ("bf16", 1900, 40, 1288, None),
          ("bf16", 64, 4096, 4096, None), ("bf16", 5, 8192, 1032, None),
-         ("mx8", 4096, 640, 2560, None), ("mx8", 4097, 672, 2568, (256, 256, 1)), ("mx8", 3900, 64, 2888, None), ("mx8", 4096, 160, 4352, None),
+         ("mx8", 4096, 640, 2560, None), ("mx8", 4097, 672, 2568, (256, 256, 1)), ("mx8", 3900, 64, 2888, None), ("mx8", 4096, 160, 4352, None), ("mx8", 8190, 736, 4096, (256, 256, 1)),
          ("mx8", 1024, 1280, 5120, None), ("mx8", 2000, 1312, 2000, None), ("mx8", 1025, 1376, 4104, (128, 128, 1)),
          ("mx8", 77, 8192, 1280, (64, 64, 6)), ("mx8", 33, 8224, 648, None), ("mx8", 4, 4128, 8200, None), ("mx8", 200, 6144, 640, None)]
 
@@ -287,7 +287,7 @@ TILES = [("bf16", 4096, 640, 2560, (256, 256, 1)), ("bf16", 4097, 648, 2568, (25
 @pytest.mark.parametrize("x_type,rows,K,N,tile", TILES)
 def test_linear_of_every_tile(x_type, rows, K, N, tile):
     y_type = "bf16" if x_type == "mx8" else x_type
-    got = tb.toma_profile_linear(tb.make_linear_desc(rows, K, N, x_type, y_type))
+    got = tb.toma_profile_linear(tb.make_linear_desc(rows, K, N, x_type, y_type, "gelu_tanh"))
     print(f"[tile] {got}", flush=True)
     assert tile is None or got == tile
     check_linear(x_type, y_type, rows, K, N, "gelu_tanh", True, True)
