@@ -70,7 +70,7 @@ struct GemmPlan { int bm, bn, nsplit; double cost; };  // cost: estimated shader
 // CU (two for the narrow tiles).  Splitting K adds a pass that reads every fp32 partial tile and
 // writes the output.
 inline GemmPlan plan_gemm_async(int M, int N, int K, int batch, int elem_size, bool may_split, bool a_ks, bool b_ks,
-                                int epi) {
+                                int epi, int first = 0 /* widest tile on offer */) {
   static const int bm[5] = {256, 256, 128, 128, 64}, bn[5] = {256, 128, 128, 64, 64};
   static const int step[3][5] = {{3230, 2200, 1230, 1000, 560},   // both operands k-contiguous
                                  {3700, 1900, 1300, 810, 560},    // one k-major
@@ -92,7 +92,7 @@ inline GemmPlan plan_gemm_async(int M, int N, int K, int batch, int elem_size, b
   int most = may_split ? 8 : 1;
   for (int pass = f32 && may_split ? 0 : 1; pass < 2; pass++) {
     best_cost = -1.0;
-    for (int i = 0; i < 5; i++) {
+    for (int i = first; i < 5; i++) {
       const long long tiles = (long long)((M + bm[i] - 1) / bm[i]) * ((N + bn[i] - 1) / bn[i]) * batch;
       for (int ns = 1; ns <= most; ns++) {
         if (ns > 1 && nk / ns < 8) break;

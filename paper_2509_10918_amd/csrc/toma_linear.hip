@@ -1,11 +1,14 @@
 // Linear layer with its epilogue, Y = act(X W + bias) + R: which kernel a shape takes, and the fp32 and small bf16 products.
 #include <algorithm>
+#include <cmath>
 
 #include "toma_linear.h"
 
 namespace toma {
 
-// fp32, and bf16 with few tiles: the tiled product of the other stages with this epilogue.
+// fp32, and bf16 with few tiles: the tiled product of the other stages with this epilogue.  That product takes whole K steps (128
+// bytes a row): the channels behind the last whole step are added from memory when the sum is at hand, before the epilogue.
+// (The register-staged kernel, which takes any K, has no K split: fp32 900 x 1000 x 1504 took it 78 us, this way 41.)
 template <typename T> struct EpiPol {
   static constexpr bool A_KS = false, B_KS = true, SPLIT_K = true, ACC_T = true;
   static constexpr int EPI = 1;
@@ -13,8 +16,8 @@ template <typename T> struct EpiPol {
   const T *In, *Wt, *bias, *R, *R2;
   T *Out;
   float *part;
-  int rows, K, N, act;
-  __device__ __forceinline__ GemmCtx setup(int) const { return GemmCtx{rows, N, K, 0, 0, 0}; }
+  int rows, K, N, act, K_steps;  // K_steps: channels in whole steps
+  __device__ __forceinline__ GemmCtx setup(int) const { return GemmCtx{rows, N, K_steps, 0, 0, 0}; }
   __device__ __forceinline__ bool a_linear(int) const { return true; }
   __device__ __forceinline__ bool b_linear(int) const { return true; }
   __device__ __forceinline__ const T *a_ptr(const GemmCtx &, int m, int k) const { return In + (size_t)m * K + k; }
@@ -31,11 +34,39 @@ template <typename T> struct EpiPol {
     store4<T>(Out + at, v);
   }
   __device__ __forceinline__ f32x4 bias4(int n) const { return bias ? load4(bias + n) : (f32x4){0.f, 0.f, 0.f, 0.f}; }
-  __device__ __forceinline__ void finish(const GemmCtx &, int m, int n, const f32x4 &v) const { put(m, n, v, bias4(n)); }
+  __device__ __forceinline__ void finish(const GemmCtx &, int m, int n, f32x4 v) const {
+    for (int k = K_steps; k < K; k++) v += to_f32(In[(size_t)m * K + k]) * load4(Wt + (size_t)k * N + n);
+    put(m, n, v, bias4(n));
+  }
+  // the channels behind the last whole step: a fragment's eight slots (k-group g: channels k + 8 g ..) straight from memory
+  template <int TM, int TN> __device__ __forceinline__ void add_tail(WaveAccT<TM, TN> &acc, int m_w, int n_w, int lane) const {
+    const int g = lane >> 4, c = lane & 15;
+    for (int k0 = K_steps; k0 < K; k0 += 32) {
+      const int k = k0 + 8 * g;
+      Frag<T> fa[TM], fb[TN];
+#pragma unroll
+      for (int i = 0; i < TM; i++) {
+        const T *src = In + (size_t)min(m_w + 16 * i + c, rows - 1) * K;
+#pragma unroll
+        for (int e = 0; e < 8; e++) fa[i].v[e] = k + e < K ? src[k + e] : from_f32<T>(0.0f);
+      }
+#pragma unroll
+      for (int j = 0; j < TN; j++) {
+        const T *src = Wt + min(n_w + 16 * j + c, N - 1);
+#pragma unroll
+        for (int e = 0; e < 8; e++) fb[j].v[e] = k + e < K ? src[(size_t)(k + e) * N] : from_f32<T>(0.0f);
+      }
+#pragma unroll
+      for (int i = 0; i < TM; i++)
+#pragma unroll
+        for (int j = 0; j < TN; j++) mma16(acc.t[i][j], fb[j], fa[i]);
+    }
+  }
   template <int TM, int TN>
-  __device__ __forceinline__ void epilogue(const GemmCtx &x, const WaveAccT<TM, TN> &acc, int m_w, int n_w,
+  __device__ __forceinline__ void epilogue(const GemmCtx &x, WaveAccT<TM, TN> &acc, int m_w, int n_w,
                                            int lane, void *) const {
     const int g = lane >> 4, c = lane & 15;
+    if (K_steps < K) add_tail<TM, TN>(acc, m_w, n_w, lane);
 #pragma unroll
     for (int j = 0; j < TN; j++) {
       const int n = n_w + 16 * j + 4 * g;
@@ -52,6 +83,16 @@ template <typename T> struct EpiPol {
 
 // the planner's and the load-to-LDS path's smallest row count (rows past the end are clamped, so fewer do as well)
 static int gemm_rows(int rows) { return std::max(rows, 8); }
+// its channels: whole steps, where there is one (else all of them, on the register-staged kernel)
+static int gemm_steps(int K, int elem_size) {
+  const int step = 128 / elem_size;
+  return K >= step ? K / step * step : K;
+}
+// its tile and K split.  256 x 256 is not on offer: with this epilogue its sums do not fit the registers (bf16 4096 x 320 x 2560:
+// 39.6 us, 16.2 on the tiled kernel; fp32 8192 x 1024 x 4096: 612 us, 540 with 256 x 128)
+static GemmPlan plan_tiles(int rows, int N, int K_steps, int elem_size) {
+  return plan_gemm_async(rows, N, K_steps, 1, elem_size, true, false, true, 1, 1);
+}
 
 // ---- which kernel --------------------------------------------------------------------------------------------------------
 // Estimated times in microseconds, fitted to measurements of every kernel on the same shapes (replayed graphs, so without host
@@ -84,6 +125,15 @@ static double rounds_cost(const RoundCost &c, const toma_linear_desc &d, int ste
   return t;
 }
 
+// What the planner's estimate leaves out of an unsplit product in bf16, per round: this epilogue, and the channels behind the last
+// whole step (strided loads, two bytes each of W).  4096 x 648 x 1280, us: 128 x 128 tiles of the tiled kernel 15.5, planned tiles
+// of 256 x 128 18.4; 4096 x 64 x 1280: 7.8 and 9.3; 4096 x 72 x 1280: 8.4 and 11.8.
+static double epilogue_cost(const GemmPlan &p, int rows, int N, bool tail) {
+  const long long wgs = (long long)((rows + p.bm - 1) / p.bm) * ((N + p.bn - 1) / p.bn);
+  const double part = std::min(p.bm * p.bn / 16384.0, 1.0);
+  return (double)((wgs + 255) / 256) * (4.25 * std::sqrt(part) + (tail ? 3.0 * part : 0.0));
+}
+
 // The fp32 partial sums of a K split are written and read once, by a kernel more.
 static double split_cost(int rows, int N, int nsplit) { return 3.0 + (8.0 * nsplit + 4.0) * rows * N / 4.0e6; }
 
@@ -104,18 +154,16 @@ static LinPlan plan_linear(const toma_linear_desc &d) {
       offer(rounds_cost(kSmall, d, (groups + ns - 1) / ns * 4, ns) + split_cost(d.rows, d.N, ns), {PATH_SMALL, 64, 64, ns});
     return best;
   }
-  const int es = d.x_type == TOMA_F32 ? 4 : 2, rows = gemm_rows(d.rows);
+  const int es = d.x_type == TOMA_F32 ? 4 : 2, rows = gemm_rows(d.rows), K = gemm_steps(d.K, es);
   LinPlan best{PATH_SMALL, 64, 64, 1};
   double least;
-  if (gemm_async_fits(rows, d.N, d.K, es)) {
-    const GemmPlan p = plan_gemm_async(rows, d.N, d.K, 1, es, true, false, true, 1);
+  if (gemm_async_fits(rows, d.N, K, es)) {
+    const GemmPlan p = plan_tiles(rows, d.N, K, es);
     best = {PATH_SMALL, p.bm, p.bn, p.nsplit};
     least = p.cost / 2100.0;
-  } else {  // the register-staged kernel: 64 x 64 tiles, one per CU at a time
-    const GemmShape g = choose_gemm_shape(rows, d.N, 1);
-    best = {PATH_SMALL, g.bm, g.bn, 1};
-    const long long wgs = (long long)((rows + 63) / 64) * ((d.N + 63) / 64);
-    least = 2.5 + (double)((wgs + 255) / 256) * 0.4 * ((d.K + 63) / 64);
+    if (d.x_type == TOMA_BF16 && p.nsplit == 1) least += epilogue_cost(p, rows, d.N, K < d.K);
+  } else {  // less than one step: the register-staged kernel
+    least = 2.5 + (double)(((long long)((rows + 63) / 64) * ((d.N + 63) / 64) + 511) / 512) * 2.0;
   }
   if (d.x_type == TOMA_BF16) {
     const int steps = (d.K + 63) / 64;
@@ -131,13 +179,33 @@ void plan_linear_tile(const toma_linear_desc &d, int32_t *out3) {
 }
 
 template <typename T>
-static void linear_typed(const LinArgs &a, float *part, hipStream_t st) {
+static void linear_typed(const LinArgs &a, const LinPlan &plan, float *part, hipStream_t st) {
   EpiPol<T> p{};
   p.In = static_cast<const T *>(a.X); p.Wt = static_cast<const T *>(a.W); p.bias = static_cast<const T *>(a.bias);
   p.R = static_cast<const T *>(a.R); p.R2 = static_cast<const T *>(a.R2); p.Out = static_cast<T *>(a.Y);
   p.part = part;
-  p.rows = a.rows; p.K = a.K; p.N = a.N; p.act = a.act;
-  launch_gemm<T>(K_LINEAR, p, gemm_rows(a.rows), a.N, a.K, 1, st);
+  p.rows = a.rows; p.K = a.K; p.N = a.N; p.act = a.act; p.K_steps = gemm_steps(a.K, (int)sizeof(T));
+  const int M = gemm_rows(a.rows), N = a.N;
+  {
+    KernelTimer kt(K_LINEAR, st);
+    const int tm = (M + plan.bm - 1) / plan.bm, tn = (N + plan.bn - 1) / plan.bn;
+    const dim3 grid(tm * tn * plan.nsplit);
+    if (!gemm_async_fits(M, N, p.K_steps, (int)sizeof(T)))
+      hipLaunchKernelGGL((k_gemm<T, EpiPol<T>, 64, 64>), grid, dim3(256), 0, st, p, tm, tn);
+    else if (plan.bm == 256)
+      hipLaunchKernelGGL((k_gemm_async<T, EpiPol<T>, 256, 128, 3>), grid, dim3(512), 0, st, p, tm, tn, 1, plan.nsplit);
+    else if (plan.bn == 128)
+      hipLaunchKernelGGL((k_gemm_async<T, EpiPol<T>, 128, 128, 4>), grid, dim3(512), 0, st, p, tm, tn, 1, plan.nsplit);
+    else if (plan.bm == 128)
+      hipLaunchKernelGGL((k_gemm_async<T, EpiPol<T>, 128, 64, 4>), grid, dim3(512), 0, st, p, tm, tn, 1, plan.nsplit);
+    else
+      hipLaunchKernelGGL((k_gemm_async<T, EpiPol<T>, 64, 64, 4>), grid, dim3(512), 0, st, p, tm, tn, 1, plan.nsplit);
+  }
+  if (plan.nsplit > 1) {
+    KernelTimer kt(K_SPLIT, st);
+    const size_t quads = (size_t)M * (N / 4);
+    hipLaunchKernelGGL((k_split_finish<T, EpiPol<T>>), dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, st, p, 1, plan.nsplit);
+  }
 }
 
 size_t linear_workspace_bytes(const toma_linear_desc &d) {
@@ -159,9 +227,9 @@ int launch_linear(const toma_linear_desc &d, const void *X, const void *Xs, cons
     KernelTimer kt(K_LINEAR, st);
     launch_linear_small(a, mx_out, plan.nsplit, part, st);
   } else if (d.x_type == TOMA_BF16) {
-    linear_typed<bf16_t>(a, part, st);
+    linear_typed<bf16_t>(a, plan, part, st);
   } else {
-    linear_typed<float>(a, part, st);
+    linear_typed<float>(a, plan, part, st);
   }
   return launch_status();
 }

@@ -276,7 +276,7 @@ def test_linear_of_many_rows(x_type, rows, K, N):
 
 
 # sizes that take each tile, whole and ragged in every extent, and those beside a change of tile
-TILES = [("bf16", 4096, 640, 2560, (256, 256, 1)), ("bf16", 4097, 648, 2568, (256, 256, 1)), ("bf16", 3900, 72, 2888, (128, 128, 1)),
+TILES = [("bf16", 4096, 640, 2560, (256, 256, 1)), ("bf16", 4097, 648, 2568, (256, 256, 1)), ("bf16", 3900, 72, 2888, (256, 256, 1)),
          ("bf16", 1024, 1280, 5120, None), ("bf16", 2000, 1288, 2000, (128, 128, 1)), ("bf16", 1025, 1344, 4104, None), ("bf16", 1900, 40, 1288, None),
          ("bf16", 64, 4096, 4096, None), ("bf16", 5, 8192, 1032, None),
          ("mx8", 4096, 640, 2560, None), ("mx8", 4097, 672, 2568, (256, 256, 1)), ("mx8", 3900, 64, 2888, None), ("mx8", 4096, 160, 4352, None), ("mx8", 8190, 736, 4096, (256, 256, 1)),
@@ -284,7 +284,14 @@ TILES = [("bf16", 4096, 640, 2560, (256, 256, 1)), ("bf16", 4097, 648, 2568, (25
          ("mx8", 77, 8192, 1280, (64, 64, 6)), ("mx8", 33, 8224, 648, None), ("mx8", 4, 4128, 8200, None), ("mx8", 200, 6144, 640, None)]
 
 
-@pytest.mark.parametrize("x_type,rows,K,N,tile", TILES)
+# channels behind the last whole step of 128 bytes, on every tile, with and without a K split
+RAGGED_K = [("bf16", 200, 72, 136, (64, 64, 1)), ("bf16", 1, 4104, 640, (64, 64, 8)), ("bf16", 63, 2040, 1000, None), ("bf16", 2858, 4656, 8, (128, 64, 8)),
+            ("bf16", 950, 1352, 1416, (128, 64, 1)), ("bf16", 1000, 4152, 1000, None), ("bf16", 134, 6344, 3608, (256, 128, 8)), ("bf16", 300, 8, 648, None),
+            ("f32", 5, 36, 12, (64, 64, 1)), ("f32", 3, 8188, 260, (64, 64, 8)), ("f32", 947, 356, 1420, None), ("f32", 400, 12, 4100, None),
+            ("f32", 1062, 40, 4104, None), ("f32", 9016, 2988, 72, (256, 128, 7)), ("f32", 66, 4044, 3400, None), ("f32", 2634, 44, 4752, None)]
+
+
+@pytest.mark.parametrize("x_type,rows,K,N,tile", TILES + RAGGED_K)
 def test_linear_of_every_tile(x_type, rows, K, N, tile):
     y_type = "bf16" if x_type == "mx8" else x_type
     got = tb.toma_profile_linear(tb.make_linear_desc(rows, K, N, x_type, y_type, "gelu_tanh"))
