@@ -125,13 +125,13 @@ static double rounds_cost(const RoundCost &c, const toma_linear_desc &d, int ste
   return t;
 }
 
-// What the planner's estimate leaves out of an unsplit product in bf16, per round: this epilogue, and the channels behind the last
-// whole step (strided loads, two bytes each of W).  4096 x 648 x 1280, us: 128 x 128 tiles of the tiled kernel 15.5, planned tiles
-// of 256 x 128 18.4; 4096 x 64 x 1280: 7.8 and 9.3; 4096 x 72 x 1280: 8.4 and 11.8.
-static double epilogue_cost(const GemmPlan &p, int rows, int N, bool tail) {
-  const long long wgs = (long long)((rows + p.bm - 1) / p.bm) * ((N + p.bn - 1) / p.bn);
-  const double part = std::min(p.bm * p.bn / 16384.0, 1.0);
-  return (double)((wgs + 255) / 256) * (4.25 * std::sqrt(part) + (tail ? 3.0 * part : 0.0));
+// What the planner's estimate, whose steps are about a tenth too long here, leaves out of an unsplit product in bf16, per round: this
+// epilogue, and the channels behind the last whole step (strided loads, two bytes each of W).  4096 x 648 x 1280, us: 128 x 128
+// tiles of the tiled kernel 15.5, planned tiles of 256 x 128 18.4; 4096 x 64 x 1280: 7.8 and 9.3; 4096 x 72 x 1280: 8.4 and 11.8.
+static double epilogue_cost(const GemmPlan &p, const toma_linear_desc &d, int rows, bool tail) {
+  const long long wgs = (long long)((rows + p.bm - 1) / p.bm) * ((d.N + p.bn - 1) / p.bn);
+  const double area = p.bm * p.bn / 16384.0, part = std::min(area, 1.0);
+  return (double)((wgs + 255) / 256) * (4.75 * std::sqrt(part) + (tail ? 3.0 * part : 0.0) + kMedium[0].act[d.act] * area);
 }
 
 // The fp32 partial sums of a K split are written and read once, by a kernel more.
@@ -161,7 +161,7 @@ static LinPlan plan_linear(const toma_linear_desc &d) {
     const GemmPlan p = plan_tiles(rows, d.N, K, es);
     best = {PATH_SMALL, p.bm, p.bn, p.nsplit};
     least = p.cost / 2100.0;
-    if (d.x_type == TOMA_BF16 && p.nsplit == 1) least += epilogue_cost(p, rows, d.N, K < d.K);
+    if (d.x_type == TOMA_BF16 && p.nsplit == 1) least = 0.9 * least + epilogue_cost(p, d, rows, K < d.K);
   } else {  // less than one step: the register-staged kernel
     least = 2.5 + (double)(((long long)((rows + 63) / 64) * ((d.N + 63) / 64) + 511) / 512) * 2.0;
   }
