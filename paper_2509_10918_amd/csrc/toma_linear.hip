@@ -113,7 +113,8 @@ static GemmPlan plan_tiles(int rows, int N, int K_steps, int elem_size) {
 struct RoundCost { int tile, slots; double fixed, full, few, act[4]; };
 constexpr RoundCost kLarge[2] = {{256, 256, 7.0, 1.4, 1.05, {0.0, 5.3, 3.0, 1.0}},     // bf16
                                  {256, 256, 7.0, 1.78, 1.3, {0.0, 5.3, 3.0, 1.0}}};    // 8 bits
-constexpr RoundCost kMedium[2] = {{128, 512, 5.0, 0.85, 0.58, {0.0, 1.9, 1.2, 0.4}}, {128, 512, 5.0, 0.9, 0.6, {0.0, 1.9, 1.2, 0.4}}};
+constexpr RoundCost kMedium[2] = {{128, 512, 5.0, 0.8, 0.55, {0.0, 1.9, 1.2, 0.4}}, {128, 512, 5.0, 0.9, 0.6, {0.0, 1.9, 1.2, 0.4}}};
+constexpr RoundCost kAlone[2] = {{128, 256, 5.0, 0.42, 0.42, {0.0, 1.9, 1.2, 0.4}}, {128, 256, 5.0, 0.54, 0.54, {0.0, 1.9, 1.2, 0.4}}};  // one a CU
 constexpr RoundCost kSmall = {64, 512, 2.5, 0.41, 0.27, {0.0, 0.6, 0.4, 0.2}};         // 8 bits
 
 static double rounds_cost(const RoundCost &c, const toma_linear_desc &d, int steps, int nsplit = 1) {
@@ -134,6 +135,12 @@ static double epilogue_cost(const GemmPlan &p, const toma_linear_desc &d, int ro
   return (double)((wgs + 255) / 256) * (4.75 * std::sqrt(part) + (tail ? 3.0 * part : 0.0) + kMedium[0].act[d.act] * area);
 }
 
+// 128 x 128 tiles, with four stages where every CU gets at most one
+static double medium_cost(int kind, const toma_linear_desc &d, int steps) {
+  const bool alone = (long long)((d.rows + 127) / 128) * ((d.N + 127) / 128) <= 256;
+  return rounds_cost(alone ? kAlone[kind] : kMedium[kind], d, steps);
+}
+
 // The fp32 partial sums of a K split are written and read once, by a kernel more.
 static double split_cost(int rows, int N, int nsplit) { return 3.0 + (8.0 * nsplit + 4.0) * rows * N / 4.0e6; }
 
@@ -148,7 +155,7 @@ static LinPlan plan_linear(const toma_linear_desc &d) {
     auto offer = [&](double t, const LinPlan &p) {
       if (t < least) { least = t; best = p; }
     };
-    offer(rounds_cost(kMedium[1], d, steps), {PATH_MEDIUM, 128, 128, 1});
+    offer(medium_cost(1, d, steps), {PATH_MEDIUM, 128, 128, 1});
     offer(rounds_cost(kSmall, d, steps), {PATH_SMALL, 64, 64, 1});
     for (int ns = 2; ns <= 8 && ns <= groups; ns++)
       offer(rounds_cost(kSmall, d, (groups + ns - 1) / ns * 4, ns) + split_cost(d.rows, d.N, ns), {PATH_SMALL, 64, 64, ns});
@@ -167,7 +174,7 @@ static LinPlan plan_linear(const toma_linear_desc &d) {
   }
   if (d.x_type == TOMA_BF16) {
     const int steps = (d.K + 63) / 64;
-    const double large = rounds_cost(kLarge[0], d, steps), medium = rounds_cost(kMedium[0], d, steps);
+    const double large = rounds_cost(kLarge[0], d, steps), medium = medium_cost(0, d, steps);
     if (std::min(large, medium) < least) best = large < medium ? LinPlan{PATH_LARGE, 256, 256, 1} : LinPlan{PATH_MEDIUM, 128, 128, 1};
   }
   return best;

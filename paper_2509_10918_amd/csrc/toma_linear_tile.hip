@@ -3,14 +3,17 @@
 // A workgroup computes BM x BN outputs, a wave WTM x WTN of them with the 16 x 16 matrix instructions (the 32 x 32 ones reach 1.79
 // instead of 2.10 PFLOP/s in bf16 on random data, 4.1 instead of 4.5 in 8 bits), the weights as first operand, so that a lane holds
 // one row and four consecutive columns of each.  K advances by 128 bytes of a row of X per step (128 channels in 8 bits, 64 in
-// bf16: whole cache lines), through two stages in LDS that the load-to-LDS path fills.
+// bf16: whole cache lines), through stages in LDS that the load-to-LDS path fills.  256 x 256 outputs and 128 x 128 take two stages,
+// one and two workgroups on a CU.  128 x 128 with at most one workgroup for every CU take four: nobody else runs while a load is on
+// its way (two and four stages, us: bf16 4096 x 2560 x 640 26.8 and 22.7, 2048 x 2048 x 2048 23.2 and 21.1; 1024 x 1280 x 5120, 320
+// workgroups, 23.7 and 28.9.  Four waves instead of eight: 29.6 and 28.8, 25.3 and 24.4, 24.7 and 35.2).
 // A 128-byte row of a stage is eight 16-byte packets; packet p of row r lies at place p ^ (r >> 1 & 7), which spreads the 16 rows
 // that a fragment read takes over all banks.
 #include "toma_linear.h"
 
 namespace toma {
 
-template <int KIND, int BM, int BN, int WM, int WN, bool MX_OUT>
+template <int KIND, int BM, int BN, int WM, int WN, int STAGES, bool MX_OUT>
 __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a, int tiles_m, int tiles_n) {
   constexpr int NW = WM * WN, WTM = BM / WM, WTN = BN / WN, TM = WTM / 16, TN = WTN / 16;
   constexpr int ES = KIND == LIN_MX ? 1 : 2, BK = 128 / ES;
@@ -21,8 +24,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a
   static_assert(TM % 4 == 0 && NIB % 2 == 0 && TN % (TM / 4) == 0, "row blocks in pairs and halves");
   static_assert(TN <= 4 && TM <= 8, "column and row blocks spelled out below");
   constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, S_BYTES = KIND == LIN_MX ? (BM + BN) * 16 : 0;
-  constexpr int SLOTS = 2;  // of four steps' codes
-  constexpr int B_AT = 2 * A_BYTES, S_AT = B_AT + 2 * B_BYTES, LDS_BYTES = S_AT + SLOTS * S_BYTES;
+  constexpr int AHEAD = STAGES - 2;  // steps that loads run ahead of what two stages allow
+  constexpr int SLOTS = AHEAD ? 4 : 2;  // of four steps' codes
+  constexpr int B_AT = STAGES * A_BYTES, S_AT = B_AT + STAGES * B_BYTES, LDS_BYTES = S_AT + SLOTS * S_BYTES;
   __shared__ __align__(1024) uint8_t lds[LDS_BYTES];
 
   int tile_m, tile_n;
@@ -156,7 +160,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a
 
   // ---- K loop -----------------------------------------------------------------------------------------------------------
   using std::integral_constant;
-  constexpr bool TURNS = NW == 8;
+  constexpr bool TURNS = BM == 256;
   auto product = [&](auto i_, auto j_, const i32x8 &x, const i32x8 &v, int e) {
     constexpr int i = decltype(i_)::value, j = decltype(j_)::value;
     if constexpr (KIND == LIN_MX) {
@@ -174,12 +178,14 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a
   // of the pairs those of W and the codes for the next step, and loads) and products.  With eight waves the two waves of a SIMD take
   // turns: a barrier stands behind every phase, and waves 4 .. 7 run one phase behind, so that one wave of a SIMD feeds the
   // matrix core while the other one waits for memory.  (Both in the same phase at the same time, the matrix cores were busy 53 % of
-  // the time: 8192^3 in 8 bits 506 us.)  With four waves two workgroups share a CU and take turns by themselves.
-  // What a phase may read or overwrite (s: step): X's lower pairs are read in the first half of the pairs, so in the second half
-  // their place takes the loads of step s + 2; the upper pairs, and W of step s + 1, in the second half: in the step behind, their
-  // places take the loads of the upper pairs of step s + 2 and W of step s + 3.  The loads are spread over the phases (28 at once
-  // kept the address unit busy for longer than a phase).  A wave waits for its loads of a half before the barrier in front of that
-  // half; every load has a step or more to land.
+  // the time: 8192^3 in 8 bits 506 us, with turns 442.)  The 128 x 128 tiles do without: two workgroups on a CU take turns by
+  // themselves, and a lone one is bound by LDS: 96 KiB of fragments and 32 KiB of loads per step at 128 bytes a clock are 1000
+  // clocks, its products 512 (bf16 4096 x 2560 x 640 with turns 24.0 us, without 22.7).
+  // What a phase may read or overwrite, with two stages (s: step; four only load two steps further ahead): X's lower pairs are read
+  // in the first half of the pairs, so in the second half their place takes the loads of step s + 2; the upper pairs, and W of step
+  // s + 1, in the second half: in the step behind, their places take the loads of the upper pairs of step s + 2 and W of step s + 3.
+  // The loads are spread over the phases (28 at once kept the address unit busy for longer than a phase).  A wave waits for its
+  // loads of a half before the barrier in front of that half; every load has a step or more to land.
   constexpr int TP = TM / 2, HP = TP / 2;
   i32x8 fx[2], fw[2][TN];
   if constexpr (KIND == LIN_MX) {
@@ -187,16 +193,16 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a
     issue_codes(0, 1);
     issue_codes(0, 2);
   }
-  next_codes(0);
-  issue_w(0, 0, lower);
-  issue_w(0, 0, upper);
-  issue_x(0, 0, lower);
-  issue_x(0, 0, upper);
-  next_codes(1);
-  issue_w(1, 1, lower);
-  issue_w(1, 1, upper);
-  issue_x(1, 1, lower);
-  wait_vmcnt<2 * NIA + NIB + NIS>();  // W and the lower half of step 0
+#pragma unroll
+  for (int j = 0; j < STAGES; j++) {
+    next_codes(j);
+    issue_w(j, j, lower);
+    issue_w(j, j, upper);
+    issue_x(j, j, lower);
+    if (j < STAGES - 1) issue_x(j, j, upper);
+  }
+  constexpr int PER_STEP = 2 * NIA + NIB + NIS, EARLY = AHEAD * PER_STEP;  // loads
+  wait_vmcnt<EARLY + PER_STEP>();  // W and the lower half of step 0
   meet();
 #pragma unroll
   for (int j = 0; j < TN; j++) fw[0][j] = read_w(j);
@@ -219,18 +225,19 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a
         if constexpr (p >= HP) {
 #pragma unroll
           for (int j = 0; j < TN; j++)
-            if (j / (TN / HP) == p - HP) fw[st ^ 1][j] = read_w(j);
+            if (j / (TN / HP) == p - HP) fw[(st + 1) & 1][j] = read_w(j);
           if constexpr (KIND == LIN_MX && p == TP - 1) read_codes(kt + 1);
         }
         if constexpr (p == 0) {
-          issue_x(st ^ 1, kt + 1, upper);
-          next_codes(kt + 2);
+          issue_x((st + STAGES - 1) % STAGES, kt + 1 + AHEAD, upper);
+          next_codes(kt + 2 + AHEAD);
         }
-        if constexpr (p == HP - 1) issue_w(st, kt + 2, lower);
-        if constexpr (p == HP) issue_w(st, kt + 2, upper);
-        if constexpr (p == TP - 1) issue_x(st, kt + 2, lower);
+        if constexpr (p == HP - 1) issue_w(st, kt + 2 + AHEAD, lower);
+        if constexpr (p == HP) issue_w(st, kt + 2 + AHEAD, upper);
+        if constexpr (p == TP - 1) issue_x(st, kt + 2 + AHEAD, lower);
         if constexpr (p == TP - 1) {  // the addresses move to the other stage
-          constexpr int da = st ? -A_BYTES : A_BYTES, db = st ? B_BYTES : -B_BYTES;
+          constexpr int da = st == STAGES - 1 ? -(STAGES - 1) * A_BYTES : A_BYTES;
+          constexpr int db = st == STAGES - 2 ? -(STAGES - 1) * B_BYTES : B_BYTES;  // (W is read a step ahead)
           rx[0] += da;
           rx[1] += da;
 #pragma unroll
@@ -239,8 +246,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (TURNS || p == HP - 1 || p == TP - 1) {
           __builtin_amdgcn_s_waitcnt(0xc07f);
-          if constexpr (p == HP - 1) wait_vmcnt<2 * NIA + NIS + NIB / 2>();
-          if constexpr (p == TP - 1) wait_vmcnt<2 * NIA + NIS + NIB>();
+          if constexpr (p == HP - 1) wait_vmcnt<EARLY + PER_STEP - NIB / 2>();
+          if constexpr (p == TP - 1) wait_vmcnt<EARLY + PER_STEP>();
           meet();
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -250,8 +257,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a
           if constexpr (j < TN) {
 #pragma unroll
             for (int e = 0; e < (KIND == LIN_MX ? 1 : 2); e++) {
-              product(integral_constant<int, 2 * p>(), j_, fx[0], fw[st][j], e);
-              product(integral_constant<int, 2 * p + 1>(), j_, fx[1], fw[st][j], e);
+              product(integral_constant<int, 2 * p>(), j_, fx[0], fw[st & 1][j], e);
+              product(integral_constant<int, 2 * p + 1>(), j_, fx[1], fw[st & 1][j], e);
             }
           }
         };
@@ -270,6 +277,12 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a
     if (++kt >= nk) break;
     step(upper, kt);
     if (++kt >= nk) break;
+    if constexpr (STAGES == 4) {
+      step(integral_constant<int, 2>(), kt);
+      if (++kt >= nk) break;
+      step(integral_constant<int, 3>(), kt);
+      if (++kt >= nk) break;
+    }
   }
   if (TURNS && w < 4) meet();
   wait_vmcnt<0>();  // (the zeros of the steps behind the last)
@@ -279,23 +292,30 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a
   linear_epilogue<TM, TN, MX_OUT>(a, acc, reinterpret_cast<float *>(lds) + w * kEpilogueFloats<TN>, m0 + wm * WTM, n0 + wn * WTN, lane);
 }
 
-template <int KIND, int BM, int BN, int WM, int WN>
+template <int KIND, int BM, int BN, int WM, int WN, int STAGES>
 static void go(const LinArgs &a, bool mx_out, hipStream_t st) {
   const int tm = (a.rows + BM - 1) / BM;
   const int tn = (a.N + BN - 1) / BN;
   const dim3 grid((unsigned)(tm * (long long)tn)), block(64 * WM * WN);
   if constexpr (KIND == LIN_MX) {
     if (mx_out) {
-      hipLaunchKernelGGL((k_linear_tile<KIND, BM, BN, WM, WN, true>), grid, block, 0, st, a, tm, tn);
+      hipLaunchKernelGGL((k_linear_tile<KIND, BM, BN, WM, WN, STAGES, true>), grid, block, 0, st, a, tm, tn);
       return;
     }
   }
-  hipLaunchKernelGGL((k_linear_tile<KIND, BM, BN, WM, WN, false>), grid, block, 0, st, a, tm, tn);
+  hipLaunchKernelGGL((k_linear_tile<KIND, BM, BN, WM, WN, STAGES, false>), grid, block, 0, st, a, tm, tn);
+}
+
+template <int KIND> static void pick(bool large, const LinArgs &a, bool mx_out, hipStream_t st) {
+  if (large) return go<KIND, 256, 256, 2, 4, 2>(a, mx_out, st);
+  const long long wgs = (long long)((a.rows + 127) / 128) * ((a.N + 127) / 128);
+  if (wgs <= 256) return go<KIND, 128, 128, 2, 4, 4>(a, mx_out, st);
+  go<KIND, 128, 128, 2, 4, 2>(a, mx_out, st);
 }
 
 void launch_linear_tile(int kind, bool large, const LinArgs &a, bool mx_out, hipStream_t st) {
-  if (kind == LIN_MX) large ? go<LIN_MX, 256, 256, 2, 4>(a, mx_out, st) : go<LIN_MX, 128, 128, 2, 2>(a, mx_out, st);
-  else large ? go<LIN_BF16, 256, 256, 2, 4>(a, mx_out, st) : go<LIN_BF16, 128, 128, 2, 2>(a, mx_out, st);
+  if (kind == LIN_MX) pick<LIN_MX>(large, a, mx_out, st);
+  else pick<LIN_BF16>(large, a, mx_out, st);
 }
 
 }  // namespace toma
