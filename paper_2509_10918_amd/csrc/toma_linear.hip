@@ -99,30 +99,33 @@ static GemmPlan plan_tiles(int rows, int N, int K_steps, int elem_size) {
 // time).  A kernel's workgroups run in rounds of what the chip holds; a round costs a fixed part (first loads, epilogue) and a part
 // per K step of 128 bytes a row, which is smaller where CUs are left over or hold one workgroup instead of two.
 // Measured and estimated, us (bf16, rows x K x N):            large        medium       planned tiles
-//   16384 x 4096 x 8192                                       790 / 778    1000 / 970   1088
-//   4096 x 640 x 2560                                         21.9 / 21.0  23.1 / 26.3  27.9 / 23.4
-//   1024 x 1280 x 5120                                        30.4 / 30.0  22.3 / 24.0  23.9 / 22.0
-//   1024 x 5120 x 1280                                        84 / 93      49 / 53      25.3 / 29.2
+//   16384 x 4096 x 8192                                       795 / 775    984 / 899    1003 / 965
+//   4096 x 640 x 2560                                         21.1 / 23.0  20.4 / 22.2  28.9 / 32.7
+//   1024 x 1280 x 5120                                        29.0 / 30.0  20.4 / 22.5  23.3 / 24.5
+//   4096 x 2560 x 640                                         47.3 / 51.0  23.2 / 23.8  23.7 / 29.6
+//   1024 x 5120 x 1280                                        83.9 / 93.0  37.3 / 40.6  24.6 / 29.2 (K split in 3)
 // and in 8 bits:                                              large        medium       small
-//   16384 x 4096 x 8192                                       521 / 513    625 / 660    -
-//   1024 x 1280 x 5120                                        23.2 / 22.0  16.5 / 16.0  20.4 / 15.2
-//   1024 x 5120 x 1280                                        59 / 61      31 / 31      21.5 / 20.9
-//   77 x 8192 x 1280                                          87 / 92      43 / 45      20.7 / 21.8, K split in 5: 11.3 / 11.2
-// few: per step where at most half of the slots are taken; act: per round for each activation (two workgroups on a CU run one's
-// epilogue beside the other's products: 16384 x 640 x 2560 in 8 bits 53 and 48 us without activation, 69 and 58 with gelu)
-struct RoundCost { int tile, slots; double fixed, full, few, act[4]; };
-constexpr RoundCost kLarge[2] = {{256, 256, 7.0, 1.4, 1.05, {0.0, 5.3, 3.0, 1.0}},     // bf16
-                                 {256, 256, 7.0, 1.78, 1.3, {0.0, 5.3, 3.0, 1.0}}};    // 8 bits
-constexpr RoundCost kMedium[2] = {{128, 512, 5.0, 0.8, 0.55, {0.0, 1.9, 1.2, 0.4}}, {128, 512, 5.0, 0.9, 0.6, {0.0, 1.9, 1.2, 0.4}}};
-constexpr RoundCost kAlone[2] = {{128, 256, 5.0, 0.42, 0.42, {0.0, 1.9, 1.2, 0.4}}, {128, 256, 5.0, 0.54, 0.54, {0.0, 1.9, 1.2, 0.4}}};  // one a CU
-constexpr RoundCost kSmall = {64, 512, 2.5, 0.41, 0.27, {0.0, 0.6, 0.4, 0.2}};         // 8 bits
+//   16384 x 4096 x 8192                                       492 / 514    616 / 541    1000 / 1002
+//   4096 x 640 x 2560                                         18.0 / 17.9  16.3 / 16.7  27.7 / 24.8
+//   1024 x 1280 x 5120                                        23.1 / 22.0  16.4 / 15.5  20.5 / 20.4
+//   1024 x 5120 x 1280                                        59.0 / 61.0  28.7 / 28.6  21.6 / 20.9 (K split in 2)
+//   77 x 8192 x 1280                                          85.9 / 92.2  38.7 / 41.6  20.6 / 21.8, K split in 5: 11.3 / 11.2
+// rest: the fixed part of a last, started round (two workgroups on a CU: it starts while the others end); few: per step where at
+// most half of the slots are taken; act: per round for each activation (two workgroups on a CU run one's epilogue beside the other's
+// products: 16384 x 640 x 2560 in 8 bits 48 and 47 us without activation, 65 and 60 with gelu)
+struct RoundCost { int tile, slots; double fixed, rest, full, few, act[4]; };
+constexpr RoundCost kLarge[2] = {{256, 256, 7.0, 7.0, 1.4, 1.05, {0.0, 5.3, 3.0, 1.0}},     // bf16
+                                 {256, 256, 7.0, 7.0, 1.78, 1.3, {0.0, 5.3, 3.0, 1.0}}};    // 8 bits
+constexpr RoundCost kMedium[2] = {{128, 512, 4.5, 2.2, 0.8, 0.5, {0.0, 1.9, 1.2, 0.4}}, {128, 512, 4.5, 2.2, 0.9, 0.6, {0.0, 1.9, 1.2, 0.4}}};
+constexpr RoundCost kAlone[2] = {{128, 256, 5.0, 5.0, 0.42, 0.42, {0.0, 1.9, 1.2, 0.4}}, {128, 256, 5.0, 5.0, 0.54, 0.54, {0.0, 1.9, 1.2, 0.4}}};
+constexpr RoundCost kSmall = {64, 512, 2.5, 2.5, 0.41, 0.27, {0.0, 0.6, 0.4, 0.2}};         // 8 bits
 
 static double rounds_cost(const RoundCost &c, const toma_linear_desc &d, int steps, int nsplit = 1) {
   const long long wgs = (long long)((d.rows + c.tile - 1) / c.tile) * ((d.N + c.tile - 1) / c.tile) * nsplit;
   const long long rest = wgs % c.slots;
-  const double fixed = c.fixed + (nsplit == 1 ? c.act[d.act] : 0.0);
-  double t = 2.0 + (double)(wgs / c.slots) * (fixed + c.full * steps);
-  if (rest) t += fixed + (2 * rest > c.slots ? c.full : c.few) * steps;
+  const double act = nsplit == 1 ? c.act[d.act] : 0.0;
+  double t = 2.0 + (double)(wgs / c.slots) * (c.fixed + act + c.full * steps);
+  if (rest) t += (wgs > c.slots ? c.rest : c.fixed) + act + (2 * rest > c.slots ? c.full : c.few) * steps;
   return t;
 }
 

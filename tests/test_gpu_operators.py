@@ -276,27 +276,36 @@ def test_linear_of_many_rows(x_type, rows, K, N):
 
 
 # sizes that take each tile, whole and ragged in every extent, and those beside a change of tile
-TILES = [("bf16", 4096, 640, 2560, (256, 256, 1)), ("bf16", 4097, 648, 2568, (256, 256, 1)), ("bf16", 3900, 72, 2888, (256, 256, 1)),
-         ("bf16", 1024, 1280, 5120, None), ("bf16", 2000, 1288, 2000, (128, 128, 1)), ("bf16", 1025, 1344, 4104, None), ("bf16", 1900, 40, 1288, None),
-         ("bf16", 64, 4096, 4096, None), ("bf16", 5, 8192, 1032, None),
-         ("mx8", 4096, 640, 2560, None), ("mx8", 4097, 672, 2568, (256, 256, 1)), ("mx8", 3900, 64, 2888, None), ("mx8", 4096, 160, 4352, None), ("mx8", 8190, 736, 4096, (256, 256, 1)),
-         ("mx8", 1024, 1280, 5120, None), ("mx8", 2000, 1312, 2000, None), ("mx8", 1025, 1376, 4104, (128, 128, 1)),
-         ("mx8", 77, 8192, 1280, (64, 64, 6)), ("mx8", 33, 8224, 648, None), ("mx8", 4, 4128, 8200, None), ("mx8", 200, 6144, 640, None)]
-
-
+TILES = [("bf16", 4096, 640, 2560), ("bf16", 4097, 648, 2568), ("bf16", 3900, 72, 2888), ("bf16", 1024, 1280, 5120), ("bf16", 2000, 1288, 2000),
+         ("bf16", 1025, 1344, 4104), ("bf16", 1900, 40, 1288), ("bf16", 64, 4096, 4096), ("bf16", 5, 8192, 1032),
+         ("bf16", 4096, 640, 4096), ("bf16", 3900, 1288, 3912), ("bf16", 2000, 64, 2000), ("bf16", 2000, 136, 2000), ("bf16", 1900, 200, 1992), ("bf16", 1900, 264, 1992),
+         ("mx8", 4096, 640, 2560), ("mx8", 4097, 672, 2568), ("mx8", 3900, 64, 2888), ("mx8", 4096, 160, 4352), ("mx8", 8190, 736, 4096),
+         ("mx8", 1024, 1280, 5120), ("mx8", 2000, 1312, 2000), ("mx8", 1025, 1376, 4104), ("mx8", 2000, 128, 2000), ("mx8", 2000, 288, 2000), ("mx8", 1900, 416, 1992),
+         ("mx8", 1900, 544, 1992), ("mx8", 77, 8192, 1280), ("mx8", 33, 8224, 648), ("mx8", 4, 4128, 8200), ("mx8", 200, 6144, 640)]
 # channels behind the last whole step of 128 bytes, on every tile, with and without a K split
-RAGGED_K = [("bf16", 200, 72, 136, (64, 64, 1)), ("bf16", 1, 4104, 640, (64, 64, 8)), ("bf16", 63, 2040, 1000, None), ("bf16", 2858, 4656, 8, (128, 64, 8)),
-            ("bf16", 950, 1352, 1416, (128, 64, 1)), ("bf16", 1000, 4152, 1000, None), ("bf16", 134, 6344, 3608, (256, 128, 8)), ("bf16", 300, 8, 648, None),
-            ("f32", 5, 36, 12, (64, 64, 1)), ("f32", 3, 8188, 260, (64, 64, 8)), ("f32", 947, 356, 1420, None), ("f32", 400, 12, 4100, None),
-            ("f32", 1062, 40, 4104, None), ("f32", 9016, 2988, 72, (256, 128, 7)), ("f32", 66, 4044, 3400, None), ("f32", 2634, 44, 4752, None)]
+RAGGED_K = [("bf16", 200, 72, 136), ("bf16", 1, 4104, 640), ("bf16", 63, 2040, 1000), ("bf16", 2858, 4656, 8), ("bf16", 950, 1352, 1416), ("bf16", 1000, 4152, 1000),
+            ("bf16", 134, 6344, 3608), ("bf16", 300, 8, 648), ("f32", 5, 36, 12), ("f32", 3, 8188, 260), ("f32", 947, 356, 1420), ("f32", 400, 12, 4100),
+            ("f32", 1062, 40, 4104), ("f32", 9016, 2988, 72), ("f32", 66, 4044, 3400), ("f32", 2634, 44, 4752)]
 
 
-@pytest.mark.parametrize("x_type,rows,K,N,tile", TILES + RAGGED_K)
-def test_linear_of_every_tile(x_type, rows, K, N, tile):
+def tile_taken(x_type, rows, K, N):
+    return tb.toma_profile_linear(tb.make_linear_desc(rows, K, N, x_type, "bf16" if x_type == "mx8" else x_type, "gelu_tanh"))
+
+
+def test_the_sizes_take_every_tile():
+    taken = {(x, *tile_taken(x, *size)[:2]) for x, *size in TILES}
+    assert taken >= {("bf16", 256, 256), ("bf16", 128, 128), ("bf16", 64, 64), ("mx8", 256, 256), ("mx8", 128, 128), ("mx8", 64, 64)}
+    assert {tile_taken(x, *size)[2] > 1 for x, *size in TILES if x == "mx8"} == {False, True}
+    ragged = {(x, *tile_taken(x, *size)) for x, *size in RAGGED_K}
+    for x in ("bf16", "f32"):
+        assert {t[1:3] for t in ragged if t[0] == x and t[3] == 1} >= {(64, 64)} and {t[1:3] for t in ragged if t[0] == x and t[3] > 1} >= {(64, 64), (256, 128)}
+    assert {t[1:3] for t in ragged if t[0] == "bf16"} >= {(128, 64)} and {t[1:3] for t in ragged if t[0] == "f32"} >= {(128, 128), (256, 128)}
+
+
+@pytest.mark.parametrize("x_type,rows,K,N", TILES + RAGGED_K)
+def test_linear_of_every_tile(x_type, rows, K, N):
     y_type = "bf16" if x_type == "mx8" else x_type
-    got = tb.toma_profile_linear(tb.make_linear_desc(rows, K, N, x_type, y_type, "gelu_tanh"))
-    print(f"[tile] {got}", flush=True)
-    assert tile is None or got == tile
+    print(f"[tile] {tile_taken(x_type, rows, K, N)}", flush=True)
     check_linear(x_type, y_type, rows, K, N, "gelu_tanh", True, True)
     if x_type == "mx8":
         check_linear(x_type, "mx8", rows, K, (N + 31) // 32 * 32, "gelu", True, False)
