@@ -284,7 +284,7 @@ int toma_mlp(int32_t dtype, int32_t rows, int32_t C, int32_t hidden, const void 
  *
  * 8-bit tensors (TOMA_MX8) are two arrays: elements Q [rows, K], one e4m3 byte each, and scale codes
  * S [rows, toma_mx_scale_stride(K)], one byte per 32 consecutive channels of a row; channel k of a row stands for
- * Q * 2^(S[k / 32] - 127).  K % 32 == 0; bytes of S behind K / 32 are written as 0 and not interpreted.  Packing takes
+ * Q * 2^(S[k / 32] - 127), for codes 0 .. 254.  K % 32 == 0; bytes of S behind K / 32 are written as 0 and not interpreted.  Packing takes
  * the smallest power of two by which the largest finite magnitude of the 32 fits 448 (2^-127 at least) and
  * rounds the quotients to the nearest e4m3, ties to even; infinities and NaN become NaN.
  *   toma_mx_quantize         X [rows, K] (x_type TOMA_F32 / TOMA_BF16) -> Q, S
@@ -302,13 +302,15 @@ int toma_mx_dequantize(int32_t y_type, int32_t rows, int32_t K, const void *Q, c
 /*
  * Root-mean-square norm with the residual's addition, per row of C channels:
  *   h = x + r;   y = h / sqrt(mean(h^2) + eps) * gamma
- * The sum and the norm are evaluated in fp32 from the unrounded h.
+ * The sum and the norm are evaluated in fp32 from the unrounded h; a row whose sum of squares passes fp32's range (one value
+ * of 2^64, or a thousand of 2^59) gives zeros, as in any fp32 evaluation of the formula.
  *   X        in   [rows, C]       x_type
  *   R_opt    in   [rows, C]       x_type; NULL: h = x
  *   gamma_opt in  [C]             x_type; NULL: 1
  *   H_opt    out  [rows, C]       h in x_type; may be X or R_opt itself; NULL: not wanted
  *   Y        out  [rows, C]       y_type; with TOMA_MX8 the elements, and Ys_opt the scale codes; overlaps no input
- * Limits: C % 32 == 0, C <= 16384, rows * max(C, 64) < 2^34; x_type TOMA_F32 / TOMA_BF16; y_type x_type or TOMA_MX8 (Ys_opt is non-NULL exactly then).
+ * Limits: C % 32 == 0, C <= 16384, rows * max(C, 64) < 2^34; x_type TOMA_F32 / TOMA_BF16; y_type x_type or TOMA_MX8 (Ys_opt
+ * is non-NULL exactly then).
  * Rows may be heads: the norm of 64-wide queries and keys is a call with C = 64 and rows = tokens * heads.
  */
 typedef struct {

@@ -283,11 +283,13 @@ class _Call:
     def __init__(self):
         self.device = torch.cuda.current_device() if torch.cuda.is_initialized() else 0
 
-    def arg(self, what, t, code, count):
-        """count: elements the tensor has to hold."""
+    def arg(self, what, t, code, count, width=0):
+        """count: elements the tensor has to hold; width: of its last dimension, where a transposed tensor would hold as many."""
         if t is None:
             return None
-        dtype = _TORCH[code]
+        dtype = _TORCH.get(code)
+        if width and t.shape[-1:] != (width,):
+            raise ValueError(f"{what}: last dimension {width} expected, got the shape {tuple(t.shape)}")
         if t.dtype is not dtype or t.numel() != count or t.get_device() != self.device or not t.is_contiguous():
             _refuse(what, t, dtype, count, self.device)
         return t.data_ptr()
@@ -376,7 +378,7 @@ def toma_linear(desc, X, Xs, W, Ws, bias, R, Y, Ys, ws):
     rows, K, N, x = desc.rows, desc.K, desc.N, desc.x_type
     e = TOMA_F32 if x == TOMA_F32 else TOMA_BF16   # bias and residual
     c = _Call()
-    _check(lib().toma_linear(_ref(desc), c.arg("X", X, x, rows * K), c.arg("Xs", Xs, TOMA_MX8, rows * _scale_stride(K)), c.arg("W", W, x, K * N),
+    _check(lib().toma_linear(_ref(desc), c.arg("X", X, x, rows * K), c.arg("Xs", Xs, TOMA_MX8, rows * _scale_stride(K)), c.arg("W", W, x, K * N, K if x == TOMA_MX8 else N),
                              c.arg("Ws", Ws, TOMA_MX8, N * _scale_stride(K)), c.arg("bias", bias, e, N), c.arg("R", R, e, rows * N),
                              c.arg("Y", Y, desc.y_type, rows * N), c.arg("Ys", Ys, TOMA_MX8, rows * _scale_stride(N)), *c.scratch(ws), c.stream()),
            "toma_linear")
@@ -400,8 +402,8 @@ def alloc_ffn_workspace(desc, device="cuda"):
 def toma_ffn(desc, X, R, gamma, W1, W1s, b1, W2, W2s, b2, Y, ws):
     C, hidden, x, w = desc.C, desc.hidden, desc.x_type, desc.w_type
     n, c = desc.rows * C, _Call()
-    _check(lib().toma_ffn(_ref(desc), c.arg("X", X, x, n), c.arg("R", R, x, n), c.arg("gamma", gamma, x, C), c.arg("W1", W1, w, C * hidden),
-                          c.arg("W1s", W1s, TOMA_MX8, hidden * _scale_stride(C)), c.arg("b1", b1, x, hidden), c.arg("W2", W2, w, C * hidden),
+    _check(lib().toma_ffn(_ref(desc), c.arg("X", X, x, n), c.arg("R", R, x, n), c.arg("gamma", gamma, x, C), c.arg("W1", W1, w, C * hidden, C if w == TOMA_MX8 else hidden),
+                          c.arg("W1s", W1s, TOMA_MX8, hidden * _scale_stride(C)), c.arg("b1", b1, x, hidden), c.arg("W2", W2, w, C * hidden, hidden if w == TOMA_MX8 else C),
                           c.arg("W2s", W2s, TOMA_MX8, C * _scale_stride(hidden)), c.arg("b2", b2, x, C), c.arg("Y", Y, x, n), *c.scratch(ws), c.stream()),
            "toma_ffn")
 

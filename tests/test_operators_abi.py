@@ -170,3 +170,36 @@ def test_packed_format_of_the_tests():
     v = ref.unpack(q, s)
     assert v[0, :3].tolist() == [448.0, 1.0, -0.3125] and v[1, 0] == 448.0 and v[1, 33] == 0.0
     assert torch.isnan(v[2, 5]) and v[2, 6] == 3.0 and v[3, 0] == 2.0 ** 127 and not v[4].any()
+
+
+def test_binding_refuses_transposed_weights():
+    """[N, K] where [K, N] is meant holds as many elements; in 8 bits it is the other way round."""
+    d, q = tb.make_linear_desc(2, 32, 64, "bf16"), tb.make_linear_desc(2, 32, 64, "mx8", "bf16")
+    x, y, w = torch.zeros(2, 32, dtype=torch.bfloat16), torch.zeros(2, 64, dtype=torch.bfloat16), torch.zeros(64, 32, dtype=torch.bfloat16)
+    u8 = lambda *shape: torch.zeros(*shape, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="W: last dimension 64"):
+        tb.toma_linear(d, _OnDevice(x), None, w, None, None, None, y, None, None)
+    with pytest.raises(ValueError, match="W: last dimension 32"):
+        tb.toma_linear(q, _OnDevice(u8(2, 32)), None, u8(32, 64), u8(64, 4), None, None, y, None, None)
+    f = tb.make_ffn_desc(2, 32, 64, 1e-6, "bf16")
+    with pytest.raises(ValueError, match="W1: last dimension 64"):
+        tb.toma_ffn(f, _OnDevice(x), None, None, w, None, None, w, None, None, torch.zeros(2, 32, dtype=torch.bfloat16), None)
+
+
+class _OnDevice:
+    """Passes the checks that a tensor on the device would."""
+
+    def __init__(self, t):
+        self.dtype, self.t = t.dtype, t
+
+    def numel(self):
+        return self.t.numel()
+
+    def get_device(self):
+        return torch.cuda.current_device() if torch.cuda.is_initialized() else 0
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return 0
