@@ -1,4 +1,5 @@
-// Linear layer with its epilogue, Y = act(X W + bias) + R: which kernel a shape takes, and the fp32 and small bf16 products.
+// Linear layer with its epilogue, Y = act(X W + bias) + R: which kernel a shape takes, the fp32 and small bf16 products, and those
+// of few rows.
 #include <algorithm>
 #include <cmath>
 
@@ -81,6 +82,109 @@ template <typename T> struct EpiPol {
   }
 };
 
+// Few rows: bound by reading W once.  W goes from memory straight into the matrix instruction's registers: a lane takes a 16-byte
+// packet of columns of KS / 4 rows of W, so tile j of the products is made of the j-th column of every packet (bf16: the rows'
+// pairs of columns are regrouped by byte permutes), and its results are packets of neighbouring columns again.  The eight waves of
+// a workgroup take the K steps in turn, each with DEPTH steps on their way, and add their sums up through LDS; K is split between
+// workgroups as well where the columns alone are too few.  RT: tiles of 16 rows.
+// One row, us, this kernel and the 64 x 64 tiles: bf16 1280 x 5120 5.8 and 7.3, 640 x 640 4.3 and 5.4, 5120 x 1280 8.3 and 8.8,
+// 4096 x 4096 9.4 and 10.0, 8192 x 8192 (134 MB) 25.5 and 23.8; fp32 1280 x 5120 8.5 and 13.9, 640 x 640 6.1 and 14.7, 4096 x 4096
+// 17.0 and 26.5, 8192 x 8192 46 and 90.  32 rows: bf16 1280 x 5120 8.5 and 7.8, 4096 x 4096 12.3 and 11.1; fp32 13.6 and 15.2, 22.2
+// and 26.7.
+template <typename T, int RT>
+__global__ __launch_bounds__(512, 2) void k_linear_few(const EpiPol<T> p, int nsplit) {
+  constexpr bool F32 = sizeof(T) == 4;
+  constexpr int EPL = 16 / sizeof(T), CG = 16 * EPL, KS = F32 ? 16 : 32, WR = KS / 4, NW = 8, DEPTH = F32 ? 6 : 4;
+  constexpr int LD = CG + 4;  // floats
+  __shared__ __align__(16) float red[NW][16 * RT][LD];
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
+  const int n0 = blockIdx.x * CG, split = blockIdx.y, steps = (p.K + KS - 1) / KS;
+  const int s0 = (int)((long long)steps * split / nsplit), s1 = (int)((long long)steps * (split + 1) / nsplit);
+  // (columns and rows behind the end repeat the last: their results are not stored)
+  const T *wp = p.Wt + min(n0 + c * EPL, p.N - EPL) + (size_t)(WR * g) * p.N;
+  const T *xp[RT];
+#pragma unroll
+  for (int t = 0; t < RT; t++) xp[t] = p.In + (size_t)min(16 * t + c, p.rows - 1) * p.K + WR * g;
+  struct Step { u32x4 w[WR], x[RT]; };
+  auto load = [&](Step &b, int s) {
+    const int k0 = s * KS;
+    if (k0 + KS <= p.K) {
+#pragma unroll
+      for (int i = 0; i < WR; i++) b.w[i] = *reinterpret_cast<const u32x4 *>(wp + (size_t)(k0 + i) * p.N);
+#pragma unroll
+      for (int t = 0; t < RT; t++) b.x[t] = *reinterpret_cast<const u32x4 *>(xp[t] + k0);
+    } else {  // a lane's channels are in or out together (K % WR == 0); those that are not there are zeros on both sides
+      const bool in = k0 + WR * g < p.K;
+#pragma unroll
+      for (int i = 0; i < WR; i++) b.w[i] = in ? *reinterpret_cast<const u32x4 *>(wp + (size_t)(k0 + i) * p.N) : (u32x4){0, 0, 0, 0};
+#pragma unroll
+      for (int t = 0; t < RT; t++) b.x[t] = in ? *reinterpret_cast<const u32x4 *>(xp[t] + k0) : (u32x4){0, 0, 0, 0};
+    }
+  };
+  f32x4 acc[RT][EPL];
+#pragma unroll
+  for (int t = 0; t < RT; t++)
+#pragma unroll
+    for (int j = 0; j < EPL; j++) acc[t][j] = (f32x4){0.f, 0.f, 0.f, 0.f};
+  auto products = [&](const Step &b) {
+    if constexpr (F32) {
+#pragma unroll
+      for (int i = 0; i < WR; i++) {
+        const f32x4 wf = __builtin_bit_cast(f32x4, b.w[i]);
+#pragma unroll
+        for (int t = 0; t < RT; t++) {
+          const f32x4 xf = __builtin_bit_cast(f32x4, b.x[t]);
+#pragma unroll
+          for (int j = 0; j < EPL; j++) acc[t][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(wf[j], xf[i], acc[t][j], 0, 0, 0);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < EPL; j++) {
+        u32x4 f;
+#pragma unroll
+        for (int q = 0; q < 4; q++) f[q] = __builtin_amdgcn_perm(b.w[2 * q + 1][j / 2], b.w[2 * q][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+        for (int t = 0; t < RT; t++)
+          acc[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), __builtin_bit_cast(bf16x8, b.x[t]), acc[t][j], 0, 0, 0);
+      }
+    }
+  };
+  Step buf[DEPTH];
+  int s = s0 + w;
+#pragma unroll
+  for (int d = 0; d < DEPTH; d++)
+    if (s + NW * d < s1) load(buf[d], s + NW * d);
+  for (; s < s1; s += NW * DEPTH) {
+#pragma unroll
+    for (int d = 0; d < DEPTH; d++)
+      if (s + NW * d < s1) {
+        products(buf[d]);
+        if (s + NW * (d + DEPTH) < s1) load(buf[d], s + NW * (d + DEPTH));
+      }
+  }
+  // a lane: row 16 t + c, columns EPL (4 g + r) + j
+#pragma unroll
+  for (int t = 0; t < RT; t++)
+    if (16 * t + c < p.rows) {
+#pragma unroll
+      for (int r = 0; r < 4; r++)
+#pragma unroll
+        for (int j = 0; j < EPL; j += 4)
+          *reinterpret_cast<f32x4 *>(&red[w][16 * t + c][EPL * (4 * g + r) + j]) = (f32x4){acc[t][j][r], acc[t][j + 1][r], acc[t][j + 2][r], acc[t][j + 3][r]};
+    }
+  __syncthreads();
+  for (int e = tid; e < p.rows * (CG / 4); e += 64 * NW) {
+    const int m = e / (CG / 4), col = e % (CG / 4) * 4, n = n0 + col;
+    if (n >= p.N) continue;
+    f32x4 v = *reinterpret_cast<const f32x4 *>(&red[0][m][col]);
+#pragma unroll
+    for (int i = 1; i < NW; i++) v += *reinterpret_cast<const f32x4 *>(&red[i][m][col]);
+    if (nsplit > 1) *reinterpret_cast<f32x4 *>(p.part + ((size_t)split * p.rows + m) * p.N + n) = v;
+    else p.put(m, n, v, p.bias4(n));
+  }
+}
+
 // the planner's and the load-to-LDS path's smallest row count (rows past the end are clamped, so fewer do as well)
 static int gemm_rows(int rows) { return std::max(rows, 8); }
 // its channels: whole steps, where there is one (else all of them, on the register-staged kernel)
@@ -147,8 +251,26 @@ static double medium_cost(int kind, const toma_linear_desc &d, int steps) {
 // The fp32 partial sums of a K split are written and read once, by a kernel more.
 static double split_cost(int rows, int N, int nsplit) { return 3.0 + (8.0 * nsplit + 4.0) * rows * N / 4.0e6; }
 
-enum Path { PATH_LARGE, PATH_MEDIUM, PATH_SMALL };
+enum Path { PATH_LARGE, PATH_MEDIUM, PATH_SMALL, PATH_FEW };
 struct LinPlan { Path path; int bm, bn, nsplit; };
+
+// Few rows: the K split by the estimated time, fitted to splits in 1, 2, 4 and 8 of the shapes above: a wave's steps one after the
+// other, or W at 7 TB/s, and the second kernel of a split.
+constexpr int few_rows(int type) { return type == TOMA_F32 ? 32 : 16; }
+static LinPlan plan_few(const toma_linear_desc &d) {
+  const bool f32 = d.x_type == TOMA_F32;
+  LinPlan best{PATH_FEW, d.rows <= 16 ? 16 : 32, f32 ? 64 : 128, 1};
+  const int steps = f32 ? (d.K + 15) / 16 : (d.K + 31) / 32, groups = (d.N + best.bn - 1) / best.bn;
+  const double step = best.bm == 32 ? 1.4 : 0.75, bytes = (f32 ? 4.0 : 2.0) * d.K * d.N;
+  double least = 1e30;
+  for (int ns = 1; ns <= 16 && (ns == 1 || 8 * ns <= steps); ns++) {
+    const int turns = ((steps + ns - 1) / ns + 7) / 8;
+    const long long rounds = ((long long)groups * ns + 255) / 256;
+    const double t = std::max(step * turns * (double)rounds, bytes / 7.0e6) + (ns > 1 ? 2.6 + 0.2 * ns + 8.0 * ns * d.rows * d.N / 4.0e6 : 0.0);
+    if (t < least) { least = t; best.nsplit = ns; }
+  }
+  return best;
+}
 
 static LinPlan plan_linear(const toma_linear_desc &d) {
   if (d.x_type == TOMA_MX8) {
@@ -164,6 +286,7 @@ static LinPlan plan_linear(const toma_linear_desc &d) {
       offer(rounds_cost(kSmall, d, (groups + ns - 1) / ns * 4, ns) + split_cost(d.rows, d.N, ns), {PATH_SMALL, 64, 64, ns});
     return best;
   }
+  if (d.rows <= few_rows(d.x_type)) return plan_few(d);
   const int es = d.x_type == TOMA_F32 ? 4 : 2, rows = gemm_rows(d.rows), K = gemm_steps(d.K, es);
   LinPlan best{PATH_SMALL, 64, 64, 1};
   double least;
@@ -196,7 +319,13 @@ static void linear_typed(const LinArgs &a, const LinPlan &plan, float *part, hip
   p.part = part;
   p.rows = a.rows; p.K = a.K; p.N = a.N; p.act = a.act; p.K_steps = gemm_steps(a.K, (int)sizeof(T));
   const int M = gemm_rows(a.rows), N = a.N;
-  {
+  if (plan.path == PATH_FEW) {
+    KernelTimer kt(K_LINEAR, st);
+    p.K_steps = a.K;
+    const dim3 grid((unsigned)((N + plan.bn - 1) / plan.bn), (unsigned)plan.nsplit);
+    if (plan.bm == 16) hipLaunchKernelGGL((k_linear_few<T, 1>), grid, dim3(512), 0, st, p, plan.nsplit);
+    else if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((k_linear_few<T, 2>), grid, dim3(512), 0, st, p, plan.nsplit);
+  } else {
     KernelTimer kt(K_LINEAR, st);
     const int tm = (M + plan.bm - 1) / plan.bm, tn = (N + plan.bn - 1) / plan.bn;
     const dim3 grid(tm * tn * plan.nsplit);
@@ -230,7 +359,7 @@ int launch_linear(const toma_linear_desc &d, const void *X, const void *Xs, cons
   const LinPlan plan = plan_linear(d);
   float *part = static_cast<float *>(ws);
   const bool mx_out = Ys != nullptr;
-  if (plan.path != PATH_SMALL) {
+  if (plan.path == PATH_LARGE || plan.path == PATH_MEDIUM) {
     KernelTimer kt(K_LINEAR, st);
     launch_linear_tile(d.x_type == TOMA_MX8 ? LIN_MX : LIN_BF16, plan.path == PATH_LARGE, a, mx_out, st);
   } else if (d.x_type == TOMA_MX8) {

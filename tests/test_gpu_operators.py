@@ -285,7 +285,14 @@ TILES = [("bf16", 4096, 640, 2560), ("bf16", 4097, 648, 2568), ("bf16", 3900, 72
 # channels behind the last whole step of 128 bytes, on every tile, with and without a K split
 RAGGED_K = [("bf16", 200, 72, 136), ("bf16", 1, 4104, 640), ("bf16", 63, 2040, 1000), ("bf16", 2858, 4656, 8), ("bf16", 950, 1352, 1416), ("bf16", 1000, 4152, 1000),
             ("bf16", 134, 6344, 3608), ("bf16", 300, 8, 648), ("f32", 5, 36, 12), ("f32", 3, 8188, 260), ("f32", 947, 356, 1420), ("f32", 400, 12, 4100),
-            ("f32", 1062, 40, 4104), ("f32", 9016, 2988, 72), ("f32", 66, 4044, 3400), ("f32", 2634, 44, 4752)]
+            ("f32", 1062, 40, 4104), ("f32", 9016, 2988, 72), ("f32", 66, 4044, 3400), ("f32", 2634, 44, 4752),
+            ("f32", 40, 8188, 260)]
+# the kernel for few rows: its row tiles, K shorter than a step, tails, K split, columns that end inside a packet group
+FEW_ROWS = [(x, rows, K + (x == "f32") * 4, N + (x == "f32") * 4) for x in ("bf16", "f32")
+            for rows, K, N in ((1, 8, 8), (1, 24, 136), (1, 8192, 128), (2, 1280, 5120), (3, 40, 4000), (5, 1032, 72), (16, 264, 264), (15, 4104, 1000),
+                               (16, 512, 16), (9, 2048, 2048))]
+FEW_ROWS += [("f32", rows, K, N) for rows, K, N in ((17, 4, 4), (17, 1300, 68), (32, 640, 640), (31, 8188, 100), (24, 36, 2004), (32, 1024, 4096))]
+FEW_ROWS += [("bf16", 17, 1032, 72), ("f32", 33, 1028, 72)]
 
 
 def tile_taken(x_type, rows, K, N):
@@ -299,10 +306,12 @@ def test_the_sizes_take_every_tile():
     ragged = {(x, *tile_taken(x, *size)) for x, *size in RAGGED_K}
     for x in ("bf16", "f32"):
         assert {t[1:3] for t in ragged if t[0] == x and t[3] == 1} >= {(64, 64)} and {t[1:3] for t in ragged if t[0] == x and t[3] > 1} >= {(64, 64), (256, 128)}
+    few = {(x, *tile_taken(x, *size)) for x, *size in FEW_ROWS}
+    assert {t[1] for t in few} >= {16, 32} and {(t[0], t[3] > 1) for t in few if t[1] == 16} == {("bf16", False), ("bf16", True), ("f32", False), ("f32", True)}
     assert {t[1:3] for t in ragged if t[0] == "bf16"} >= {(128, 64)} and {t[1:3] for t in ragged if t[0] == "f32"} >= {(128, 128), (256, 128)}
 
 
-@pytest.mark.parametrize("x_type,rows,K,N", TILES + RAGGED_K)
+@pytest.mark.parametrize("x_type,rows,K,N", TILES + RAGGED_K + FEW_ROWS)
 def test_linear_of_every_tile(x_type, rows, K, N):
     y_type = "bf16" if x_type == "mx8" else x_type
     print(f"[tile] {tile_taken(x_type, rows, K, N)}", flush=True)
