@@ -179,8 +179,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a
   // turns: a barrier stands behind every phase, and waves 4 .. 7 run one phase behind, so that one wave of a SIMD feeds the
   // matrix core while the other one waits for memory.  (Both in the same phase at the same time, the matrix cores were busy 53 % of
   // the time: 8192^3 in 8 bits 506 us, with turns 442.)  The 128 x 128 tiles do without: two workgroups on a CU take turns by
-  // themselves, and a lone one is bound by LDS: 96 KiB of fragments and 32 KiB of loads per step at 128 bytes a clock are 1000
-  // clocks, its products 512 (bf16 4096 x 2560 x 640 with turns 24.0 us, without 22.7).
+  // themselves, and a lone one gains nothing (bf16 4096 x 2560 x 640 with turns 24.0 us, without 22.7).  A lone one takes 0.42 us a
+  // step where its products take 0.21; four waves with fewer fragment reads, fragments read a step ahead between the products, one
+  // barrier a step (23.3 us) left that as it is.
   // What a phase may read or overwrite, with two stages (s: step; four only load two steps further ahead): X's lower pairs are read
   // in the first half of the pairs, so in the second half their place takes the loads of step s + 2; the upper pairs, and W of step
   // s + 1, in the second half: in the step behind, their places take the loads of the upper pairs of step s + 2 and W of step s + 3.
