@@ -110,6 +110,18 @@ __device__ __forceinline__ uint32_t gather_bytes(const uint32_t *d, int n, uint3
   const uint32_t hi = n > 2 ? __builtin_amdgcn_perm(n > 3 ? d[3] & mask : 0u, d[2] & mask, sel) : 0u;
   return (lo & 0xffffu) | hi << 16;
 }
+// Turns a 4 x 4 matrix of bytes over between a word's bytes and the four lane groups: byte b of the result is byte g of the word
+// of lane group b (same lane of the group).  Halves of the wave first: a word's two bytes for either group of the half, from
+// both halves' words; then the groups of a half.
+__device__ __forceinline__ uint32_t turn_selector(int k) {  // bytes k, k + 1 of the second and of the first operand, alternating
+  return (uint32_t)k * 0x01010101u + 0x05010400u;
+}
+__device__ __forceinline__ uint32_t turn_bytes(uint32_t d, uint32_t pairs, uint32_t own) {
+  const auto h = __builtin_amdgcn_permlane32_swap(d, d, false, false);
+  const uint32_t p = __builtin_amdgcn_perm(h[1], h[0], pairs);
+  const auto r = __builtin_amdgcn_permlane16_swap(p, p, false, false);
+  return __builtin_amdgcn_perm(r[1], r[0], own);
+}
 // place of packet pi of k-row k in a k-major stage of PPR packets a row: four rows of 32 bytes that a transpose read takes together
 // fall on the four quarters of 256 bytes, the rows eight further on (the upper half of the wave) on what they leave
 template <int PPR> __device__ __forceinline__ int km_place(int k, int pi) {

@@ -133,23 +133,26 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a
       return join_halves(f[0], f[1]);
     }
   };
-  // scale codes of a step: byte b of word q is the code of row block 4 q + b for this lane's block of 32 channels (g)
+  // scale codes of a step: byte b of word q is the code of row block 4 q + b for this lane's block of 32 channels (g); read as a
+  // word per row (its four blocks) by lane group b, then turned over between the lane groups
   constexpr int QX = (TM + 3) / 4, QW = (TN + 3) / 4;
-  uint32_t cx[QX], cw[QW], raw_x[TM], raw_w[TN];
+  uint32_t cx[QX], cw[QW], raw_x[QX], raw_w[QW];
+  const int block_x = 16 * (g % TM), block_w = 16 * (g % TN);
   auto read_codes = [&](int j) {  // of step j
     const lds_ptr at = (lds_ptr)(lds + S_AT) + ((j >> 2) % SLOTS * S_BYTES + (j & 3) * 4) + c * 16;
 #pragma unroll
-    for (int i = 0; i < TM; i++) raw_x[i] = *(lds_u32_ptr)(at + (wm * WTM + 16 * i) * 16);
+    for (int q = 0; q < QX; q++) raw_x[q] = *(lds_u32_ptr)(at + (wm * WTM + 64 * q + block_x) * 16);
 #pragma unroll
-    for (int i = 0; i < TN; i++) raw_w[i] = *(lds_u32_ptr)(at + (BM + wn * WTN + 16 * i) * 16);
+    for (int q = 0; q < QW; q++) raw_w[q] = *(lds_u32_ptr)(at + (BM + wn * WTN + 64 * q + block_w) * 16);
   };
   const uint32_t tail_mask = K % 128 ? 0xffffffffu >> (32 - (K >> 5) % 4 * 8) : 0u;  // codes of the last group that stand for channels
+  const uint32_t turn_pairs = turn_selector(g & 2), turn_own = turn_selector((g & 1) * 2);
   auto gather_codes = [&](int j) {  // of step j
     const uint32_t mask = j < (K >> 7) ? 0xffffffffu : j == (K >> 7) ? tail_mask : 0u;
 #pragma unroll
-    for (int q = 0; q < QX; q++) cx[q] = gather_bytes(raw_x + 4 * q, TM - 4 * q, mask, g);
+    for (int q = 0; q < QX; q++) cx[q] = turn_bytes(raw_x[q] & mask, turn_pairs, turn_own);
 #pragma unroll
-    for (int q = 0; q < QW; q++) cw[q] = gather_bytes(raw_w + 4 * q, TN - 4 * q, mask, g);
+    for (int q = 0; q < QW; q++) cw[q] = turn_bytes(raw_w[q] & mask, turn_pairs, turn_own);
   };
 
   f32x4 acc[TM][TN];
