@@ -209,17 +209,17 @@ static GemmPlan plan_tiles(int rows, int N, int K_steps, int elem_size) {
 //   4096 x 2560 x 640                                         47.3 / 51.0  23.2 / 23.8  23.7 / 29.6
 //   1024 x 5120 x 1280                                        83.9 / 93.0  37.3 / 40.6  24.6 / 29.2 (K split in 3)
 // and in 8 bits:                                              large        medium       small
-//   16384 x 4096 x 8192                                       492 / 514    616 / 541    1000 / 1002
-//   4096 x 640 x 2560                                         18.0 / 17.9  16.3 / 16.7  27.7 / 24.8
-//   1024 x 1280 x 5120                                        23.1 / 22.0  16.4 / 15.5  20.5 / 20.4
-//   1024 x 5120 x 1280                                        59.0 / 61.0  28.7 / 28.6  21.6 / 20.9 (K split in 2)
-//   77 x 8192 x 1280                                          85.9 / 92.2  38.7 / 41.6  20.6 / 21.8, K split in 5: 11.3 / 11.2
+//   16384 x 4096 x 8192                                       484 / 493    616 / 535    1000 / 1002
+//   4096 x 640 x 2560                                         17.6 / 17.5  16.3 / 16.2  27.9 / 24.8
+//   1024 x 1280 x 5120                                        22.4 / 21.5  15.9 / 15.5  20.1 / 20.4
+//   1024 x 5120 x 1280                                        56.5 / 59.0  27.7 / 28.6  21.3 / 20.9 (K split in 2)
+//   77 x 8192 x 1280                                          82.4 / 89.0  36.1 / 41.6  20.6 / 21.8, K split in 5: 11.3 / 11.2
 // rest: the fixed part of a last, started round (two workgroups on a CU: it starts while the others end); few: per step where at
 // most half of the slots are taken; act: per round for each activation (two workgroups on a CU run one's epilogue beside the other's
 // products: 16384 x 640 x 2560 in 8 bits 48 and 47 us without activation, 65 and 60 with gelu)
 struct RoundCost { int tile, slots; double fixed, rest, full, few, act[4]; };
 constexpr RoundCost kLarge[2] = {{256, 256, 7.0, 7.0, 1.4, 1.05, {0.0, 5.3, 3.0, 1.0}},     // bf16
-                                 {256, 256, 7.0, 7.0, 1.78, 1.3, {0.0, 5.3, 3.0, 1.0}}};    // 8 bits
+                                 {256, 256, 7.0, 7.0, 1.7, 1.25, {0.0, 5.3, 3.0, 1.0}}};    // 8 bits
 constexpr RoundCost kMedium[2] = {{128, 512, 4.5, 2.2, 0.8, 0.5, {0.0, 1.9, 1.2, 0.4}}, {128, 512, 4.5, 2.2, 0.9, 0.6, {0.0, 1.9, 1.2, 0.4}}};
 constexpr RoundCost kAlone[2] = {{128, 256, 5.0, 5.0, 0.42, 0.42, {0.0, 1.9, 1.2, 0.4}}, {128, 256, 5.0, 5.0, 0.54, 0.54, {0.0, 1.9, 1.2, 0.4}}};
 constexpr RoundCost kSmall = {64, 512, 2.5, 2.5, 0.41, 0.27, {0.0, 0.6, 0.4, 0.2}};         // 8 bits

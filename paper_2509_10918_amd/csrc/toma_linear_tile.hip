@@ -134,7 +134,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a
     }
   };
   // scale codes of a step: byte b of word q is the code of row block 4 q + b for this lane's block of 32 channels (g); read as a
-  // word per row (its four blocks) by lane group b, then turned over between the lane groups
+  // word per row (its four blocks) by lane group b, then turned over between the lane groups (8192^3 425 us; every lane reading
+  // the words of all its row blocks, four times as many LDS reads, 447)
   constexpr int QX = (TM + 3) / 4, QW = (TN + 3) / 4;
   uint32_t cx[QX], cw[QW], raw_x[QX], raw_w[QW];
   const int block_x = 16 * (g % TM), block_w = 16 * (g % TN);
@@ -181,7 +182,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a
   // of the pairs those of W and the codes for the next step, and loads) and products.  With eight waves the two waves of a SIMD take
   // turns: a barrier stands behind every phase, and waves 4 .. 7 run one phase behind, so that one wave of a SIMD feeds the
   // matrix core while the other one waits for memory.  (Both in the same phase at the same time, the matrix cores were busy 53 % of
-  // the time: 8192^3 in 8 bits 506 us, with turns 442.)  The 128 x 128 tiles do without: two workgroups on a CU take turns by
+  // the time: 8192^3 in 8 bits 506 us, with turns 442 then.)  The 128 x 128 tiles do without: two workgroups on a CU take turns by
   // themselves, and a lone one gains nothing (bf16 4096 x 2560 x 640 with turns 24.0 us, without 22.7).  A lone one takes 0.42 us a
   // step where its products take 0.21; four waves with fewer fragment reads, fragments read a step ahead between the products, one
   // barrier a step (23.3 us) left that as it is.
