@@ -537,3 +537,96 @@ def test_pre_norm_block_on_merged_tokens(w_type):
     dv.O.copy_(y.reshape(dv.O.shape))
     Y = dv.unmerge()
     assert torch.isfinite(torch.as_tensor(Y)).all()
+
+
+# ---- tensors of more than 2^31 elements, and scratch that graphs share ---------------------------------------------------------
+
+FAR = 2 ** 21 + 37   # rows; times 1024 channels more than 2^31 elements
+
+
+def far_rows(t):
+    """A few rows: the first, those about 2^31 elements (2^20 .. 2^21 rows of 1024 channels), the last."""
+    return torch.tensor([0, 1, 2 ** 20 - 1, 2 ** 20, 2 ** 20 + 300, 2 ** 21 - 1, 2 ** 21, 2 ** 21 + 1, t - 2, t - 1], device="cuda")
+
+
+def far_values(rows, C, dtype):
+    t = torch.empty(rows, C, dtype=dtype, device="cuda")
+    t.normal_(generator=gen(rows + C))
+    return t
+
+
+@pytest.mark.parametrize("x_type", ["bf16", "f32", "mx8"])
+@pytest.mark.parametrize("K,N", [(1024, 32), (32, 1024)])
+def test_linear_beyond_32_bit_offsets(x_type, K, N):
+    e = torch.float32 if x_type == "f32" else torch.bfloat16
+    x, w, i = far_values(FAR, K, e), (randn(gen(1), K, N) * K ** -0.5).to(e), far_rows(FAR)
+    xs = ws = None
+    x64, w64 = x[i].double(), w.double()
+    if x_type == "mx8":
+        q, wq = tb.alloc_mx(FAR, K), tb.alloc_mx(N, K)
+        tb.toma_mx_quantize(x, *q)
+        tb.toma_mx_quantize_weight(w, *wq)
+        assert torch.equal(q[0][i], ref.pack(x[i])[0]) and torch.equal(q[1][i], ref.pack(x[i])[1])
+        (x, xs), (w, ws) = q, wq
+        x64, w64 = ref.unpack(q[0][i], q[1][i]), ref.unpack(*wq).t()
+    y = torch.empty(FAR, N, dtype=e, device="cuda")
+    d = tb.make_linear_desc(FAR, K, N, x_type, "bf16" if x_type == "mx8" else x_type)
+    tb.toma_linear(d, x, xs, w, ws, None, None, y, None, tb.alloc_linear_workspace(d))
+    want = x64 @ w64
+    tol = (x64.abs() @ w64.abs()) * (K * 2.0 ** -24 + (2.0 ** -12 if x_type == "mx8" else 0.0)) + EPI * want.abs()
+    within(y[i], want, (want.abs() + tol) * HALF[e] + tol)
+
+
+@pytest.mark.parametrize("out", ["", "mx8"])
+def test_norm_beyond_32_bit_offsets(out):
+    C, i = 1024, far_rows(FAR)
+    x, g = far_values(FAR, C, torch.bfloat16), randn(gen(2), C).to(torch.bfloat16)
+    r = x[:1].expand(FAR, C).contiguous()
+    h = torch.empty_like(x)
+    want_h, want = ref.norm(x[i], r[i], g, 1e-6)
+    d = tb.make_norm_desc(FAR, C, 1e-6, "bf16", out or "bf16")
+    y = tb.alloc_mx(FAR, C) if out else (torch.empty_like(x), None)
+    tb.toma_rmsnorm(d, x, r, g, h, *y)
+    within(h[i], want_h, want_h.abs() * HALF[torch.bfloat16])
+    if not out:
+        return within(y[0][i], want, want.abs() * (HALF[torch.bfloat16] + C * 2.0 ** -24 + EPI))
+    back = torch.empty_like(x)
+    tb.toma_mx_dequantize(*y, back)
+    assert torch.equal(back[i].double(), ref.unpack(y[0][i], y[1][i]))
+    tol = want.abs() * (C * 2.0 ** -24 + EPI)
+    sc = torch.exp2(y[1][i][:, :C // 32].double() - 127).repeat_interleave(32, 1)
+    within(back[i], want, (want.abs() + tol) * 2.0 ** -4 + sc * 2.0 ** -10 + tol)
+
+
+def test_graphs_that_share_scratch_in_order():
+    """Two captured calls with a K split each and one scratch between them, replayed one after the other on one stream, eager calls
+    with the same scratch in between."""
+    shapes = [("f32", 3, 4096, 512, "gelu"), ("bf16", 64, 8192, 512, "silu"), ("mx8", 77, 8192, 1280, "none")]
+    calls, graphs = [], []
+    descs = [tb.make_linear_desc(r, K, N, x, "bf16" if x == "mx8" else x, a) for x, r, K, N, a in shapes]
+    assert all(tb.toma_profile_linear(d)[2] > 1 for d in descs)
+    ws = torch.empty(max(tb.toma_linear_workspace_bytes(d) for d in descs), dtype=torch.uint8, device="cuda")
+    for d, (x_type, rows, K, N, act) in zip(descs, shapes):
+        x, w, b, r, _, _ = linear_case(x_type, "", rows, K, N, act, True, True)
+        y = torch.empty(rows, N, dtype=torch.float32 if x_type == "f32" else torch.bfloat16, device="cuda")
+        calls.append((lambda d=d, x=x, w=w, b=b, r=r, y=y: tb.toma_linear(d, x[0], x[1], w[0], w[1], b, r, y, None, ws), y))
+    want = []
+    for call, y in calls:
+        call()
+        torch.cuda.synchronize()
+        want.append(y.clone())
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            call()
+    for k in range(3):
+        for _, y in calls:
+            y.zero_()
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(y, v) for (_, y), v in zip(calls, want)), k
+        for call, y in calls:
+            y.zero_()
+            call()
+        torch.cuda.synchronize()
+        assert all(torch.equal(y, v) for (_, y), v in zip(calls, want)), k
