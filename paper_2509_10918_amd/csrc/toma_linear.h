@@ -7,7 +7,6 @@
 namespace toma {
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 // X [rows, K], W [K, N] (8-bit: [N, K]); Xs, Ws, Ys: scale codes; R, R2: residuals (R2: a second one, of the feed-forward block)
 struct LinArgs {

@@ -11,21 +11,12 @@
 
 namespace toma {
 
-// N loads of 1 KiB each to consecutive KiB of LDS behind lds_addr, from one buffer; off[t] carries 4096 - 1024 t on top (the
+// Two loads of 1 KiB each to consecutive KiB of LDS behind lds_addr, from one buffer; off[t] carries 4096 - 1024 t on top (the
 // instruction's immediate adds 1024 t to both addresses; the buffer's base lies 4096 below).
-template <int N>
-__device__ __forceinline__ void buffer_to_lds_run(const uint8_t *base, uint32_t bytes, const uint32_t (&off)[N], uint32_t lds_addr) {
-  static_assert(N == 1 || N == 2 || N == 4, "spelled out");
+__device__ __forceinline__ void buffer_to_lds_pair(const uint8_t *base, uint32_t bytes, const uint32_t (&off)[2], uint32_t lds_addr) {
   const u32x4 rsrc = buffer_of(base - 4096, bytes);
-  if constexpr (N == 1)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds_addr), "v"(off[0]), "s"(rsrc) : "memory", "m0");
-  else if constexpr (N == 2)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %3, 0 offen lds\n\tbuffer_load_dwordx4 %2, %3, 0 offen offset:1024 lds" ::"s"(lds_addr),
-                 "v"(off[0]), "v"(off[1]), "s"(rsrc) : "memory", "m0");
-  else
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %5, 0 offen lds\n\tbuffer_load_dwordx4 %2, %5, 0 offen offset:1024 lds\n\t"
-                 "buffer_load_dwordx4 %3, %5, 0 offen offset:2048 lds\n\tbuffer_load_dwordx4 %4, %5, 0 offen offset:3072 lds" ::"s"(lds_addr),
-                 "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(rsrc) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %3, 0 offen lds\n\tbuffer_load_dwordx4 %2, %3, 0 offen offset:1024 lds" ::"s"(lds_addr),
+               "v"(off[0]), "v"(off[1]), "s"(rsrc) : "memory", "m0");
 }
 
 // RAGGED: K is no multiple of a step
@@ -98,8 +89,8 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_small(const LinArgs a, 
       for (int t = 0; t < NIA; t++) ox[t] = !RAGGED || xk[t] < K - j * BK ? xo[t] : kNoPacket;
 #pragma unroll
       for (int t = 0; t < NIB; t++) ow[t] = !RAGGED || wk[t] < K - j * BK ? wo[t] : kNoPacket;
-      buffer_to_lds_run<NIA>(xb + (size_t)j * 128, bytes, ox, lx + (uint32_t)((2 * slot + h) * A_BYTES));
-      buffer_to_lds_run<NIB>(wb + (size_t)j * 128, bytes, ow, lw + (uint32_t)((2 * slot + h) * B_BYTES));
+      buffer_to_lds_pair(xb + (size_t)j * 128, bytes, ox, lx + (uint32_t)((2 * slot + h) * A_BYTES));
+      buffer_to_lds_pair(wb + (size_t)j * 128, bytes, ow, lw + (uint32_t)((2 * slot + h) * B_BYTES));
     }
   };
 

@@ -87,7 +87,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a
   // end of K, and all of a step behind the last, are zeros that nothing is read for.
   auto issue_x = [&](uint32_t st, int j, auto upper_) {
     constexpr int h = decltype(upper_)::value;
-    const uint32_t bytes = j < nk ? 0x40000000u : 0u;
+    const uint32_t bytes = j < nk ? kAllPackets : 0u;
     const int left = K - j * BK;
 #pragma unroll
     for (int t = 0; t < NIA; t++) {
@@ -97,7 +97,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_linear_tile(const LinArgs a
   };
   auto issue_w = [&](uint32_t st, int j, auto half_) {
     constexpr int h = decltype(half_)::value;
-    const uint32_t bytes = j < nk ? 0x40000000u : 0u;
+    const uint32_t bytes = j < nk ? kAllPackets : 0u;
     const int left = K - j * BK;
 #pragma unroll
     for (int t = h * NIB / 2; t < (h + 1) * NIB / 2; t++) {

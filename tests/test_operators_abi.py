@@ -104,7 +104,7 @@ def test_linear_tile_is_host_arithmetic():
         for rows, K, N in ((16384, 4096, 8192), (1025, 1376, 4104), (512, 640, 640), (77, 8192, 1280), (1, 8192, 640)):
             d = tb.make_linear_desc(rows, K, N, x_type, y_type)
             bm, bn, split = tb.toma_profile_linear(d)
-            assert bm in (64, 128, 256) and bn in (64, 128, 256) and 1 <= split <= 8
+            assert bm in (16, 32, 64, 128, 256) and bn in (64, 128, 256) and 1 <= split <= (16 if bm <= 32 else 8)
             need = tb.toma_linear_workspace_bytes(d)
             assert need == 0 if split == 1 else need >= 4 * split * rows * N
             seen.add((x_type, bm, bn, split > 1))
