@@ -17,7 +17,17 @@ struct NormArgs {
   uint8_t *Ys;
   int rows, C, stride;  // stride: scale codes per row
   float eps;
+  double inv_C;     // 1 / C
 };
+
+// What a row shares is kept to more than fp32's accuracy: its squares are summed in fp32 eight at a time and in fp64 from there
+// on, and the inverse root takes a Newton step in fp64.  Of 42 million packed outputs 20 instead of 25 then lie on the other side of
+// a rounding border from the exact ones, at the same time within 1 %.
+__device__ __forceinline__ float inverse_root(double v) {
+  const float f = 1.0f / sqrtf((float)v);
+  const double d = (double)f, n = d * (1.5 - 0.5 * v * d * d);
+  return v < 3.0e38 ? (float)n : f;  // (past fp32's range: 0)
+}
 
 // L lanes share a row, each holding NP packets of eight channels (packet p of lane l: channels 8 (L p + l) ..): a wave's loads
 // then cover 16 L consecutive bytes per row and packet, and all of a lane's loads are on their way together (up to eight of x and
@@ -45,39 +55,39 @@ __global__ __launch_bounds__(256) void k_rmsnorm(const NormArgs a) {
 #pragma unroll
       for (int i = 0; i < 8; i++) h[p].v[i] += r[p].v[i];
   }
-  float sum = 0.0f;
+  double sum = 0.0;
 #pragma unroll
   for (int p = 0; p < NP; p++) {
     float s = 0.0f;
 #pragma unroll
     for (int i = 0; i < 8; i++) s = __builtin_fmaf(h[p].v[i], h[p].v[i], s);
-    if (L * p + l < packets) sum += s;
+    if (L * p + l < packets) sum += (double)s;
   }
 #pragma unroll
-  for (int m = 1; m < (L < 64 ? L : 64); m *= 2) sum += wave_xor_f32(sum, m);
+  for (int m = 1; m < (L < 64 ? L : 64); m *= 2) sum += wave_xor_f64(sum, m);
   if constexpr (L > 64) {
-    __shared__ float part[L / 64];
+    __shared__ double part[L / 64];
     if ((tid & 63) == 0) part[tid >> 6] = sum;
     __syncthreads();
-    sum = 0.0f;
+    sum = 0.0;
 #pragma unroll
     for (int i = 0; i < L / 64; i++) sum += part[i];
   }
   if (!live) return;  // (the quads of a row go on together)
-  const float f = 1.0f / sqrtf(sum / (float)a.C + a.eps);
+  const float f = inverse_root(sum * a.inv_C + (double)a.eps);
 #pragma unroll
   for (int p = 0; p < NP; p++) {
     const int q = L * p + l;
     const bool in = q < packets;
     if (H && in) store8(H + base + 8 * q, h[p]);
     F8 y = h[p];
-#pragma unroll
-    for (int i = 0; i < 8; i++) y.v[i] *= f;
-    if (G) {
+    if (G) {  // (bf16: h gamma is exact unless x and r are more than eight powers of two apart)
       const F8 g = load8(G + 8 * min(q, packets - 1));
 #pragma unroll
       for (int i = 0; i < 8; i++) y.v[i] *= g.v[i];
     }
+#pragma unroll
+    for (int i = 0; i < 8; i++) y.v[i] *= f;
     if constexpr (MX) {
       u32x2 o;
       const uint32_t code = mx_pack_quad(y, o);  // (C % 32 == 0: a quad is in or out as a whole)
@@ -119,7 +129,7 @@ static void launch_norm_typed(const NormArgs &a, hipStream_t st) {
 
 int launch_rmsnorm(const toma_norm_desc &d, const void *X, const void *R, const void *gamma, void *H, void *Y, void *Ys,
                    hipStream_t st) {
-  NormArgs a{X, R, gamma, H, Y, static_cast<uint8_t *>(Ys), d.rows, d.C, mx_scale_stride(d.C), d.eps};
+  NormArgs a{X, R, gamma, H, Y, static_cast<uint8_t *>(Ys), d.rows, d.C, mx_scale_stride(d.C), d.eps, 1.0 / d.C};
   KernelTimer kt(K_NORM, st);
   const bool mx = d.y_type == TOMA_MX8;
   if (d.x_type == TOMA_BF16) mx ? launch_norm_typed<bf16_t, true>(a, st) : launch_norm_typed<bf16_t, false>(a, st);
