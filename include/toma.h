@@ -302,8 +302,8 @@ int toma_mx_dequantize(int32_t y_type, int32_t rows, int32_t K, const void *Q, c
 /*
  * Root-mean-square norm with the residual's addition, per row of C channels:
  *   h = x + r;   y = h / sqrt(mean(h^2) + eps) * gamma
- * The sum and the norm are evaluated in fp32 from the unrounded h; a row whose sum of squares passes fp32's range (one value
- * of 2^64, or a thousand of 2^59) gives zeros, as in any fp32 evaluation of the formula.
+ * The sum and the norm are evaluated in fp32 or more from the unrounded h.  h * gamma and the sum of the squares of eight
+ * neighbouring channels have to be in fp32's range: a row whose squares pass it (one value of 2^64) gives zeros.
  *   X        in   [rows, C]       x_type
  *   R_opt    in   [rows, C]       x_type; NULL: h = x
  *   gamma_opt in  [C]             x_type; NULL: 1
