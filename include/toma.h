@@ -330,7 +330,8 @@ int toma_rmsnorm(const toma_norm_desc *desc, const void *X, const void *R_opt, c
  *   bias_opt  in   [N]         fp32 products: fp32; else bf16
  *   R_opt     in   [rows, N]   as bias; may be Y itself
  *   Y         out  [rows, N]   y_type (TOMA_MX8: elements, Ys_opt their scale codes); overlaps no other input
- * Products accumulate in fp32, the epilogue is evaluated in fp32 and rounded once.
+ * Products accumulate in fp32, the epilogue is evaluated in fp32 and rounded once.  For bf16 and packed outputs TOMA_ACT_GELU is a
+ * fit in fp32, off by at most 2^-14 of its value (toma_mlp's takes the error function); -inf gives NaN, as the formulas do.
  * Types: x_type TOMA_F32 / TOMA_BF16 with y_type the same; x_type TOMA_MX8 with y_type TOMA_BF16 or TOMA_MX8.
  * Limits: TOMA_F32: K % 4 == 0, N % 4 == 0; TOMA_BF16: K % 8 == 0, N % 8 == 0; TOMA_MX8: K % 32 == 0 and N % 8 == 0 (y_type
  * TOMA_MX8: N % 32 == 0).  K, N <= 2^20, rows <= 2^28, rows * max(K, N) < 2^34, K * N < 2^31.

@@ -18,19 +18,22 @@ struct LinArgs {
   int rows, K, N, act, xs_stride, ys_stride;
 };
 
-// Activations.  fp32 outputs: to fp32 accuracy.  bf16 and 8-bit outputs (half a step is 2^-9 of the value at best): gelu with the
-// normal tail Q(a) = 1 - Phi(a) = exp(-a^2 / 2) P(1 / (1 + 0.38 a)), P of degree 5 fitted to a relative error of 2^-14.8 over all
-// a >= 0, as x Phi(x) = x / 2 + |x| (1/2 - Q(|x|)): 12 instructions and two transcendental ones instead of the error function's
-// about 60, with which a 256 x 256 tile's epilogue was as long as ten K steps.
+// Activations.  fp32 outputs: gelu by the complementary error function.  bf16 and 8-bit outputs (half a step is 2^-9 of the value at
+// best): v Phi(v) with Phi(v) = |s - Q(|v|)|, s = 1 for v > 0 and else 0, and the normal tail Q(a) = exp(-a^2 / 2) P(1 / (1 + 0.38 a)),
+// the form of Hastings' approximations, P of degree 5 fitted to a relative error of 2^-14.8 over all a >= 0; nothing cancels, and the
+// result is off by 2^-14.3 of itself at most down to v = -12.  (As v / 2 + |v| (1/2 - Q) it was off by 4 % at -5 and zero from -5.75
+// on.)  11 instructions and two transcendental ones instead of the error function's about 60, with which a 256 x 256 tile's
+// epilogue was as long as ten K steps.
 template <bool F32> __device__ __forceinline__ float gelu_f32(float v) {
-  if constexpr (F32) return 0.5f * v * (1.0f + erff(v * 0.70710678118654752f));
-  const float a = __builtin_fabsf(v), t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.38f, a, 1.0f));
+  if constexpr (F32) return 0.5f * v * erfcf(v * -0.70710678118654752f);
+  const float k = v * 0.84932180028802f;  // sqrt(log2(e) / 2)
+  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.44741580910612f, __builtin_fabsf(k), 1.0f));  // 0.38 |v|
   float p = __builtin_fmaf(-0.08992693573f, t, 0.18887339532f);
   p = __builtin_fmaf(p, t, 0.09198205173f);
   p = __builtin_fmaf(p, t, 0.15782876313f);
   p = __builtin_fmaf(p, t, 0.15122520924f);
-  const float e = __builtin_amdgcn_exp2f(v * v * -0.72134752044448f);  // -log2(e) / 2
-  return __builtin_fmaf(a, __builtin_fmaf(-(p * t), e, 0.5f), 0.5f * v);
+  const float e = __builtin_amdgcn_exp2f(-(k * k)), s = __builtin_amdgcn_fmed3f(v * 0x1p126f, 0.0f, 1.0f);
+  return v * __builtin_fabsf(__builtin_fmaf(-(p * t), e, s));
 }
 // v / (1 + exp(-u))
 __device__ __forceinline__ float gate_f32(float v, float u) {

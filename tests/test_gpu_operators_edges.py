@@ -1,0 +1,78 @@
+"""The norm, linear and packing operators on the GPU where values are far out: tails of the activations, infinities and NaN, the ends of
+the number ranges, and every kernel of the linear layer by its name.  Tolerances as in test_gpu_operators.py, relative to the
+output wherever the inputs of the last step are exact."""
+import pytest
+import torch
+
+from paper_2509_10918_amd import binding as tb
+
+import operators_ref as ref
+from test_gpu_operators import DT, HALF, NAN, check_norm, gen, linear_case, randn, run_linear, within
+
+pytestmark = pytest.mark.gpu
+INF = float("inf")
+
+
+def act64(v, name):
+    """The activations without cancellation: v Phi(v) by the complementary error function, the others by a logistic function."""
+    if name == "gelu":
+        return 0.5 * v * torch.special.erfc(-v / 2 ** 0.5)   # (torch.special.ndtr is (1 + erf) / 2: off by 2 % at -7.8)
+    if name == "gelu_tanh":
+        return v * torch.sigmoid(2 * (2 / torch.pi) ** 0.5 * (v + 0.044715 * v ** 3))
+    return v * torch.sigmoid(v) if name == "silu" else v
+
+
+# ---- activations where they are small against their argument ----------------------------------------------------------------
+
+def selecting_case(x_type, rows, K, N, lo, hi):
+    """x with values from lo to hi, and weights that pick one channel of x for every column: the pre-activations are values of x, exactly
+    (sums of one product and zeros)."""
+    g = gen(rows + K + N)
+    x = lo + (hi - lo) * torch.rand(rows, K, generator=g, device="cuda")
+    k = torch.arange(N, device="cuda") % K
+    w = torch.zeros(K, N, device="cuda")
+    w[k, torch.arange(N, device="cuda")] = 1.0
+    if x_type == "mx8":
+        x, w = ref.pack(x.to(torch.bfloat16)), ref.pack(w.t().contiguous())
+        return x, w, ref.unpack(*x)[:, k]
+    x = x.to(DT[x_type])
+    return (x, None), (w.to(DT[x_type]), None), x.double()[:, k]
+
+
+# one size for each kernel, K split and none
+SELECTING = [("bf16", 5, 64, 136), ("bf16", 3, 4096, 640), ("bf16", 200, 72, 136), ("bf16", 64, 4096, 256), ("bf16", 2000, 136, 2000), ("bf16", 4096, 640, 2560),
+             ("bf16", 40, 24, 72), ("f32", 5, 64, 136), ("f32", 3, 8188, 260), ("f32", 947, 352, 1416), ("f32", 66, 4044, 136), ("f32", 40, 12, 72),
+             ("mx8", 5, 64, 136), ("mx8", 77, 8192, 1280), ("mx8", 2000, 128, 2000), ("mx8", 1024, 1280, 5120), ("mx8", 4096, 640, 2560)]
+
+
+@pytest.mark.parametrize("act,lo,hi", [("gelu", -8.0, -3.0), ("gelu", -12.0, 3.0), ("gelu_tanh", -9.0, 3.0), ("silu", -80.0, 3.0)])
+@pytest.mark.parametrize("x_type,rows,K,N", [c for c in SELECTING if c[0] != "f32"])
+def test_tails_of_the_activations(x_type, rows, K, N, act, lo, hi):
+    """Relative to the output: the fitted gelu is off by 2^-14.8 of v Q(|v|), and the exponentials' arguments, up to 116 powers of
+    two here, by a few 2^-24 of themselves: 2^-14 in all, then half a step of the output."""
+    print(f"[tail] {x_type} {rows} x {K} x {N} {act} {lo} .. {hi}", flush=True)
+    x, w, v = selecting_case(x_type, rows, K, N, lo, hi)
+    want = act64(v, act)
+    for y_type in ("bf16", "mx8") if x_type == "mx8" else (x_type,):
+        if y_type == "mx8" and N % 32:
+            continue
+        y, s = run_linear(x_type, y_type, x, w, None, None, act)
+        if y_type == "mx8":
+            sc = torch.exp2(s[:, :N // 32].double() - 127).repeat_interleave(32, 1)
+            within(ref.unpack(y, s), want, want.abs() * (1 + 2.0 ** -14) * 2.0 ** -4 + want.abs() * 2.0 ** -14 + sc * 2.0 ** -10)
+        else:
+            within(y, want, want.abs() * (2.0 ** -8 + 2.0 ** -14 * (1 + 2.0 ** -8)))
+
+
+@pytest.mark.parametrize("lo,hi", [(-8.0, -3.0), (-12.0, 3.0)])
+@pytest.mark.parametrize("x_type,rows,K,N", [c for c in SELECTING if c[0] == "f32"])
+def test_tail_of_gelu_in_fp32(x_type, rows, K, N, lo, hi):
+    """v erfc(-v / sqrt 2) / 2: the argument has two roundings (the factor's and the product's, 2^-24 each at most), and an error of d
+    in it changes the result by (v^2 + 1) d at most; erfc has four units in the last place (2^-21), the products less."""
+    print(f"[tail] {x_type} {rows} x {K} x {N} {lo} .. {hi}", flush=True)
+    x, w, v = selecting_case(x_type, rows, K, N, lo, hi)
+    y, _ = run_linear(x_type, x_type, x, w, None, None, "gelu")
+    want = act64(v, "gelu")
+    within(y, want, want.abs() * (2.0 ** -23 * (v * v + 1) + 2.0 ** -20))
+
+
