@@ -35,8 +35,11 @@ template <bool F32> __device__ __forceinline__ float gelu_f32(float v) {
   const float e = __builtin_amdgcn_exp2f(-(k * k)), s = __builtin_amdgcn_fmed3f(v * 0x1p126f, 0.0f, 1.0f);
   return v * __builtin_fabsf(__builtin_fmaf(-(p * t), e, s));
 }
-// v / (1 + exp(-u))
-__device__ __forceinline__ float gate_f32(float v, float u) {
+// v / (1 + exp(-u)).  fp32 outputs: by the library's exponential and quotient.  The exponential instruction's argument, u log2(e) rounded,
+// is off by a few |u| 2^-24 (silu 16 times fp32's accuracy at -20), and a reciprocal below 2^-126 comes as zero (silu from -87.3 on);
+// both are far below half a step of bf16.
+template <bool F32> __device__ __forceinline__ float gate_f32(float v, float u) {
+  if constexpr (F32) return v / (1.0f + expf(-u));
   return v * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u * -1.4426950408889634f));
 }
 template <bool F32, int N> __device__ __forceinline__ void activate(float (&v)[N], int act) {  // act: the same for all lanes
@@ -47,10 +50,10 @@ template <bool F32, int N> __device__ __forceinline__ void activate(float (&v)[N
     // x/2 (1 + tanh(u)) = x / (1 + exp(-2u)), u = sqrt(2/pi) (x + 0.044715 x^3)
 #pragma unroll
     for (int i = 0; i < N; i++)
-      v[i] = gate_f32(v[i], v[i] * __builtin_fmaf(0.0713548162726f * v[i], v[i], 1.5957691216057308f));
+      v[i] = gate_f32<F32>(v[i], v[i] * __builtin_fmaf(0.0713548162726f * v[i], v[i], 1.5957691216057308f));
   } else if (act == TOMA_ACT_SILU) {
 #pragma unroll
-    for (int i = 0; i < N; i++) v[i] = gate_f32(v[i], v[i]);
+    for (int i = 0; i < N; i++) v[i] = gate_f32<F32>(v[i], v[i]);
   }
 }
 __device__ __forceinline__ f32x4 load4(const float *p) { return *reinterpret_cast<const f32x4 *>(p); }

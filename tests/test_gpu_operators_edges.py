@@ -76,3 +76,16 @@ def test_tail_of_gelu_in_fp32(x_type, rows, K, N, lo, hi):
     within(y, want, want.abs() * (2.0 ** -23 * (v * v + 1) + 2.0 ** -20))
 
 
+@pytest.mark.parametrize("act,lo,hi", [("silu", -80.0, 3.0), ("silu", -88.5, -80.0), ("gelu_tanh", -9.5, -8.0)])
+@pytest.mark.parametrize("x_type,rows,K,N", [c for c in SELECTING if c[0] == "f32"])
+def test_logistic_gates_in_fp32(x_type, rows, K, N, act, lo, hi):
+    """fp32 to fp32 accuracy: v / (1 + e^-u) has the exponential's one unit in the last place (2^-23), the sum's and the quotient's
+    roundings (2^-24 each), to which u's own come (gelu_tanh: a product of three with a constant and an addition: five)."""
+    print(f"[gate] {x_type} {rows} x {K} x {N} {act} {lo} .. {hi}", flush=True)
+    x, w, v = selecting_case(x_type, rows, K, N, lo, hi)
+    want = act64(v, act)
+    y, _ = run_linear(x_type, x_type, x, w, None, None, act)
+    u = 2 * (2 / torch.pi) ** 0.5 * (v + 0.044715 * v ** 3)
+    within(y, want, want.abs() * 2.0 ** -24 * (5 + (5 * u.abs() if act == "gelu_tanh" else 0)) * (1 + 2.0 ** -10))
+
+
