@@ -87,10 +87,12 @@ template <typename T> struct EpiPol {
 // pairs of columns are regrouped by byte permutes), and its results are packets of neighbouring columns again.  The eight waves of
 // a workgroup take the K steps in turn, each with DEPTH steps on their way, and add their sums up through LDS; K is split between
 // workgroups as well where the columns alone are too few.  RT: tiles of 16 rows.
-// One row, us, this kernel and the 64 x 64 tiles: bf16 1280 x 5120 5.8 and 7.3, 640 x 640 4.3 and 5.4, 5120 x 1280 8.3 and 8.8,
-// 4096 x 4096 9.4 and 10.0, 8192 x 8192 (134 MB) 25.5 and 23.8; fp32 1280 x 5120 8.5 and 13.9, 640 x 640 6.1 and 14.7, 4096 x 4096
-// 17.0 and 26.5, 8192 x 8192 46 and 90.  32 rows: bf16 1280 x 5120 8.5 and 7.8, 4096 x 4096 12.3 and 11.1; fp32 13.6 and 15.2, 22.2
-// and 26.7.
+// Taken for every call of up to 16 rows (fp32: 32), by the row count alone.  One row, us, this kernel and the 64 x 64 tiles (K split
+// planned): bf16 1280 x 5120 5.8 and 7.3, 640 x 640 4.3 and 5.4, 5120 x 1280 8.3 and 8.8; fp32 1280 x 5120 8.5 and 13.9, 640 x 640 6.1
+// and 14.7, 4096 x 4096 17.0 and 26.5, 8192 x 8192 46 and 82.  32 rows: fp32 1280 x 5120 11.7 and 14.4, 8192 x 8192 56 and 82; bf16
+// 1280 x 5120 8.5 and 7.8.  In bf16 the rule is not the faster one for large weights: 1 x 4096 x 4096 9.8 and 9.5, 16 rows 11.2
+// and 9.6; 1 x 8192 x 8192 (134 MB) 25.5 and 23.4; 16 x 20480 x 5120 49 and 37, but 4 x 5120 x 20480 34 and 37.  The planner's estimate
+// of the tiles is not fitted to so few rows, so the two are not weighed against each other.
 template <typename T, int RT>
 __global__ __launch_bounds__(512, 2) void k_linear_few(const EpiPol<T> p, int nsplit) {
   constexpr bool F32 = sizeof(T) == 4;
@@ -185,9 +187,7 @@ __global__ __launch_bounds__(512, 2) void k_linear_few(const EpiPol<T> p, int ns
   }
 }
 
-// the planner's and the load-to-LDS path's smallest row count (rows past the end are clamped, so fewer do as well)
-static int gemm_rows(int rows) { return std::max(rows, 8); }
-// its channels: whole steps, where there is one (else all of them, on the register-staged kernel)
+// the load-to-LDS path's channels: whole steps, where there is one (else all of them, on the register-staged kernel)
 static int gemm_steps(int K, int elem_size) {
   const int step = 128 / elem_size;
   return K >= step ? K / step * step : K;
@@ -287,7 +287,7 @@ static LinPlan plan_linear(const toma_linear_desc &d) {
     return best;
   }
   if (d.rows <= few_rows(d.x_type)) return plan_few(d);
-  const int es = d.x_type == TOMA_F32 ? 4 : 2, rows = gemm_rows(d.rows), K = gemm_steps(d.K, es);
+  const int es = d.x_type == TOMA_F32 ? 4 : 2, rows = d.rows, K = gemm_steps(d.K, es);
   LinPlan best{PATH_SMALL, 64, 64, 1};
   double least;
   if (gemm_async_fits(rows, d.N, K, es)) {
@@ -318,7 +318,7 @@ static void linear_typed(const LinArgs &a, const LinPlan &plan, float *part, hip
   p.R = static_cast<const T *>(a.R); p.R2 = static_cast<const T *>(a.R2); p.Out = static_cast<T *>(a.Y);
   p.part = part;
   p.rows = a.rows; p.K = a.K; p.N = a.N; p.act = a.act; p.K_steps = gemm_steps(a.K, (int)sizeof(T));
-  const int M = gemm_rows(a.rows), N = a.N;
+  const int M = a.rows, N = a.N;
   if (plan.path == PATH_FEW) {
     KernelTimer kt(K_LINEAR, st);
     p.K_steps = a.K;
@@ -349,7 +349,7 @@ static void linear_typed(const LinArgs &a, const LinPlan &plan, float *part, hip
 
 size_t linear_workspace_bytes(const toma_linear_desc &d) {
   const LinPlan p = plan_linear(d);
-  return p.nsplit > 1 ? (size_t)p.nsplit * gemm_rows(d.rows) * d.N * sizeof(float) : 0;
+  return p.nsplit > 1 ? (size_t)p.nsplit * d.rows * d.N * sizeof(float) : 0;
 }
 
 int launch_linear(const toma_linear_desc &d, const void *X, const void *Xs, const void *W, const void *Ws, const void *bias,
