@@ -266,12 +266,36 @@ _TYPE = {torch.float32: TOMA_F32, torch.bfloat16: TOMA_BF16, "f32": TOMA_F32, "b
 _TORCH = {TOMA_F32: torch.float32, TOMA_BF16: torch.bfloat16, TOMA_MX8: torch.uint8}
 
 
-def _refuse(what, t, dtype, count, device):
+_ROWS, _WEIGHT, _CODES = range(3)   # what a tensor is
+
+
+def _whole_rows(shape, width, several):
+    """Whether a contiguous tensor of this shape is rows of `width` one after the other: its last dimensions are one row, it is flat, or
+    (several) its last dimension is more than one row: the norm of single heads."""
+    n = 1
+    for s in reversed(shape):
+        n *= s
+        if n == width:
+            return True
+    return len(shape) == 1 or (several and len(shape) > 0 and shape[-1] % width == 0)
+
+
+def _check_layout(what, t, dtype, shape, kind, device):
+    """For a tensor that is not exactly of the expected shape, type and device: refuses it, unless it is the same rows under another
+    shape (weights: any whose last dimension is right)."""
+    count = 1
+    for n in shape:
+        count *= n
+    if kind == _WEIGHT and t.shape[-1:] != shape[-1:]:
+        raise ValueError(f"{what}: last dimension {shape[-1]} expected, got the shape {tuple(t.shape)}")
     if t.dtype is not dtype or t.numel() != count:
         raise ValueError(f"{what}: {count} elements of {dtype} expected, got {t.numel()} of {t.dtype}")
-    if not (t.is_cuda and t.is_contiguous()):
+    if len(shape) > 1 and not _whole_rows(t.shape, shape[-1], kind == _ROWS):
+        raise ValueError(f"{what}: rows of {shape[-1]} expected, got the shape {tuple(t.shape)}")
+    if t.get_device() < 0 or not t.is_contiguous():
         raise ValueError(f"{what}: libtoma takes contiguous CUDA tensors")
-    raise ValueError(f"{what} lies on {t.device}, the current device is cuda:{device}")
+    if t.get_device() != device:
+        raise ValueError(f"{what} lies on {t.device}, the current device is cuda:{device}")
 
 
 class _Call:
@@ -283,20 +307,21 @@ class _Call:
     def __init__(self):
         self.device = torch.cuda.current_device() if torch.cuda.is_initialized() else 0
 
-    def arg(self, what, t, code, count, width=0):
-        """count: elements the tensor has to hold; width: of its last dimension, where a transposed tensor would hold as many."""
+    def arg(self, what, t, code, shape, kind=_ROWS):
+        """shape: (rows, width) or (width,)"""
         if t is None:
             return None
         dtype = _TORCH.get(code)
-        if width and t.shape[-1:] != (width,):
-            raise ValueError(f"{what}: last dimension {width} expected, got the shape {tuple(t.shape)}")
-        if t.dtype is not dtype or t.numel() != count or t.get_device() != self.device or not t.is_contiguous():
-            _refuse(what, t, dtype, count, self.device)
+        if t.shape != shape or t.dtype is not dtype or t.get_device() != self.device or not t.is_contiguous():
+            _check_layout(what, t, dtype, shape, kind, self.device)
         return t.data_ptr()
+
+    def codes(self, what, t, rows, width):
+        return self.arg(what, t, TOMA_MX8, (rows, _scale_stride(width)), _CODES)
 
     def scratch(self, ws):
         """Pointer and bytes of a scratch tensor (None: no scratch)."""
-        return (None, 0) if ws is None else (self.arg("ws", ws, TOMA_MX8, ws.numel()), ws.numel())
+        return (None, 0) if ws is None else (self.arg("ws", ws, TOMA_MX8, (ws.numel(),)), ws.numel())
 
     def stream(self):
         return torch._C._cuda_getCurrentRawStream(self.device)
@@ -319,30 +344,30 @@ def alloc_mx(rows, K, device="cuda"):
             torch.empty((rows, stride), dtype=torch.uint8, device=device))
 
 
-def _pack_call(name, plain, code, rows, K, lead, Q, S):
+def _pack_call(name, what, plain, shape, code, lead, rows, K, Q, S):
     c = _Call()
-    p = c.arg("Y" if name == "toma_mx_dequantize" else "W" if name == "toma_mx_quantize_weight" else "X", plain, max(code, 0), rows * K)
-    q, s = c.arg("Q", Q, TOMA_MX8, rows * K), c.arg("S", S, TOMA_MX8, rows * _scale_stride(K))
-    args = (q, s, p) if name == "toma_mx_dequantize" else (p, q, s)
+    p = c.arg(what, plain, max(code, 0), shape)
+    q, s = c.arg("Q", Q, TOMA_MX8, (rows, K)), c.codes("S", S, rows, K)
+    args = (q, s, p) if what == "Y" else (p, q, s)
     _check(getattr(lib(), name)(code, *lead, *args, c.stream()), name)
 
 
 def toma_mx_quantize(X, Q, S):
     """X [..., K] -> Q [rows, K], S [rows, stride] (alloc_mx)."""
     rows, K = Q.shape
-    _pack_call("toma_mx_quantize", X, _TYPE.get(X.dtype, -1), rows, K, (rows, K), Q, S)
+    _pack_call("toma_mx_quantize", "X", X, (rows, K), _TYPE.get(X.dtype, -1), (rows, K), rows, K, Q, S)
 
 
 def toma_mx_quantize_weight(W, Q, S):
     """W [K, N] -> Q [N, K], S [N, stride] (alloc_mx(N, K))."""
     K, N = W.shape
-    _pack_call("toma_mx_quantize_weight", W, _TYPE.get(W.dtype, -1), N, K, (K, N), Q, S)
+    _pack_call("toma_mx_quantize_weight", "W", W, (K, N), _TYPE.get(W.dtype, -1), (K, N), N, K, Q, S)
 
 
 def toma_mx_dequantize(Q, S, Y):
     """The values of Q [rows, K], S as Y [..., K] (float32 or bfloat16)."""
     rows, K = Q.shape
-    _pack_call("toma_mx_dequantize", Y, _TYPE.get(Y.dtype, -1), rows, K, (rows, K), Q, S)
+    _pack_call("toma_mx_dequantize", "Y", Y, (rows, K), _TYPE.get(Y.dtype, -1), (rows, K), rows, K, Q, S)
 
 
 def make_norm_desc(rows, C, eps, x_type, y_type=None):
@@ -350,10 +375,11 @@ def make_norm_desc(rows, C, eps, x_type, y_type=None):
 
 
 def toma_rmsnorm(desc, X, R, gamma, H, Y, Ys=None):
+    """X, R, H, Y: rows of C, under any leading dimensions (or several rows in the last: heads)."""
     rows, C, x = desc.rows, desc.C, desc.x_type
-    n, c = rows * C, _Call()
-    _check(lib().toma_rmsnorm(_ref(desc), c.arg("X", X, x, n), c.arg("R", R, x, n), c.arg("gamma", gamma, x, C), c.arg("H", H, x, n),
-                              c.arg("Y", Y, desc.y_type, n), c.arg("Ys", Ys, TOMA_MX8, rows * _scale_stride(C)), c.stream()),
+    n, c = (rows, C), _Call()
+    _check(lib().toma_rmsnorm(_ref(desc), c.arg("X", X, x, n), c.arg("R", R, x, n), c.arg("gamma", gamma, x, (C,)), c.arg("H", H, x, n),
+                              c.arg("Y", Y, desc.y_type, n), c.codes("Ys", Ys, rows, C), c.stream()),
            "toma_rmsnorm")
 
 
@@ -378,9 +404,10 @@ def toma_linear(desc, X, Xs, W, Ws, bias, R, Y, Ys, ws):
     rows, K, N, x = desc.rows, desc.K, desc.N, desc.x_type
     e = TOMA_F32 if x == TOMA_F32 else TOMA_BF16   # bias and residual
     c = _Call()
-    _check(lib().toma_linear(_ref(desc), c.arg("X", X, x, rows * K), c.arg("Xs", Xs, TOMA_MX8, rows * _scale_stride(K)), c.arg("W", W, x, K * N, K if x == TOMA_MX8 else N),
-                             c.arg("Ws", Ws, TOMA_MX8, N * _scale_stride(K)), c.arg("bias", bias, e, N), c.arg("R", R, e, rows * N),
-                             c.arg("Y", Y, desc.y_type, rows * N), c.arg("Ys", Ys, TOMA_MX8, rows * _scale_stride(N)), *c.scratch(ws), c.stream()),
+    w = c.arg("W", W, x, (N, K) if x == TOMA_MX8 else (K, N), _WEIGHT)
+    _check(lib().toma_linear(_ref(desc), c.arg("X", X, x, (rows, K)), c.codes("Xs", Xs, rows, K), w,
+                             c.codes("Ws", Ws, N, K), c.arg("bias", bias, e, (N,)), c.arg("R", R, e, (rows, N)),
+                             c.arg("Y", Y, desc.y_type, (rows, N)), c.codes("Ys", Ys, rows, N), *c.scratch(ws), c.stream()),
            "toma_linear")
 
 
@@ -401,10 +428,12 @@ def alloc_ffn_workspace(desc, device="cuda"):
 
 def toma_ffn(desc, X, R, gamma, W1, W1s, b1, W2, W2s, b2, Y, ws):
     C, hidden, x, w = desc.C, desc.hidden, desc.x_type, desc.w_type
-    n, c = desc.rows * C, _Call()
-    _check(lib().toma_ffn(_ref(desc), c.arg("X", X, x, n), c.arg("R", R, x, n), c.arg("gamma", gamma, x, C), c.arg("W1", W1, w, C * hidden, C if w == TOMA_MX8 else hidden),
-                          c.arg("W1s", W1s, TOMA_MX8, hidden * _scale_stride(C)), c.arg("b1", b1, x, hidden), c.arg("W2", W2, w, C * hidden, hidden if w == TOMA_MX8 else C),
-                          c.arg("W2s", W2s, TOMA_MX8, C * _scale_stride(hidden)), c.arg("b2", b2, x, C), c.arg("Y", Y, x, n), *c.scratch(ws), c.stream()),
+    n, c = (desc.rows, C), _Call()
+    up, down = ((hidden, C), (C, hidden)) if w == TOMA_MX8 else ((C, hidden), (hidden, C))
+    w1, w2 = c.arg("W1", W1, w, up, _WEIGHT), c.arg("W2", W2, w, down, _WEIGHT)
+    _check(lib().toma_ffn(_ref(desc), c.arg("X", X, x, n), c.arg("R", R, x, n), c.arg("gamma", gamma, x, (C,)), w1,
+                          c.codes("W1s", W1s, hidden, C), c.arg("b1", b1, x, (hidden,)), w2,
+                          c.codes("W2s", W2s, C, hidden), c.arg("b2", b2, x, (C,)), c.arg("Y", Y, x, n), *c.scratch(ws), c.stream()),
            "toma_ffn")
 
 
