@@ -395,6 +395,8 @@ int toma_profile_map_product(const toma_desc *desc, int which, int32_t *out3);
 /* Tile and K split that toma_linear takes for this descriptor: out3 = {rows per workgroup, columns, K split}.  Host arithmetic
  * only. */
 int toma_profile_linear(const toma_linear_desc *desc, int32_t *out3);
+/* And the kernel: "few_rows", "small", "planned", "short", "medium", "medium_four_stages" or "large"; NULL for an invalid descriptor. */
+const char *toma_profile_linear_kernel(const toma_linear_desc *desc);
 /* toma_select (Sec. 4.1, Alg. 2) with the greedy kernel replaced by a variant of itself that also
  * adds up, per wave, the shader clocks spent in each part of a round - a measurement aid for the one
  * kernel whose time is a chain of dependent steps rather than bytes or products.  idx as toma_select.

@@ -21,7 +21,7 @@ EXPORTS = ("toma_workspace_bytes", "toma_status_string", "toma_select", "toma_se
            "toma_unmerge_recompute", "toma_layer", "toma_mlp", "toma_mx_scale_stride", "toma_mx_quantize", "toma_mx_quantize_weight",
            "toma_mx_dequantize", "toma_rmsnorm", "toma_linear_workspace_bytes", "toma_linear", "toma_ffn_workspace_bytes", "toma_ffn",
            "toma_profile_enable",
-           "toma_profile_kernel_name", "toma_profile_read", "toma_profile_map_product", "toma_profile_linear",
+           "toma_profile_kernel_name", "toma_profile_read", "toma_profile_map_product", "toma_profile_linear", "toma_profile_linear_kernel",
            "toma_profile_greedy_parts")
 
 
@@ -117,6 +117,8 @@ def lib():
         L.toma_linear.argtypes = [vp] * 10 + [sz, vp]
         L.toma_ffn.argtypes = [vp] * 12 + [sz, vp]
         L.toma_profile_linear.argtypes = [vp, ctypes.POINTER(ctypes.c_int32)]
+        L.toma_profile_linear_kernel.restype = ctypes.c_char_p
+        L.toma_profile_linear_kernel.argtypes = [vp]
         for name in ("toma_profile_linear", "toma_mx_quantize", "toma_mx_quantize_weight", "toma_mx_dequantize", "toma_rmsnorm", "toma_linear", "toma_ffn"):
             getattr(L, name).restype = ctypes.c_int
         for name in ("toma_select", "toma_merge", "toma_map_build", "toma_merge_cached", "toma_attend", "toma_cross_attend", "toma_unmerge", "toma_unmerge_pinv", "toma_recompute_cache_bytes", "toma_merge_recompute",
@@ -471,6 +473,12 @@ def toma_profile_linear(desc):
     out = (ctypes.c_int32 * 3)()
     _check(lib().toma_profile_linear(_ref(desc), out), "toma_profile_linear")
     return tuple(out)
+
+
+def toma_profile_linear_kernel(desc):
+    """Name of the kernel that toma_linear takes for this descriptor; None for an invalid one."""
+    name = lib().toma_profile_linear_kernel(_ref(desc))
+    return None if name is None else name.decode()
 
 
 def toma_profile_greedy_parts(desc, X, idx, parts, ws):

@@ -535,6 +535,10 @@ TOMA_API int toma_profile_linear(const toma_linear_desc *desc, int32_t *out3) {
   return TOMA_OK;
 }
 
+TOMA_API const char *toma_profile_linear_kernel(const toma_linear_desc *desc) {
+  return check_linear(desc) == TOMA_OK ? linear_kernel_name(*desc) : nullptr;
+}
+
 // The stages of a feed-forward block and where their outputs lie in the workspace.
 struct FfnPlan {
   toma_norm_desc norm;

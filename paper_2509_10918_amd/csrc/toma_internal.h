@@ -258,6 +258,7 @@ int launch_rmsnorm(const toma_norm_desc &d, const void *X, const void *R, const 
                    hipStream_t st);
 size_t linear_workspace_bytes(const toma_linear_desc &d);
 void plan_linear_tile(const toma_linear_desc &d, int32_t *out3);  // tile and K split
+const char *linear_kernel_name(const toma_linear_desc &d);
 // R2: a second residual (the feed-forward block's stream is X + R in its last epilogue)
 int launch_linear(const toma_linear_desc &d, const void *X, const void *Xs, const void *W, const void *Ws, const void *bias,
                   const void *R, const void *R2, void *Y, void *Ys, void *ws, hipStream_t st);

@@ -194,6 +194,9 @@ __device__ __forceinline__ void linear_epilogue(const LinArgs &a, const f32x4 (&
   }
 }
 
+// 128 x 128 tiles, at most one for every CU: four stages instead of two
+inline bool medium_alone(int rows, int N) { return (long long)((rows + 127) / 128) * ((N + 127) / 128) <= 256; }
+
 // part: fp32 scratch [nsplit][rows][N] when nsplit > 1
 void launch_linear_small(const LinArgs &a, bool mx_out, int nsplit, float *part, hipStream_t st);
 void launch_linear_tile(int kind, bool large, const LinArgs &a, bool mx_out, hipStream_t st);

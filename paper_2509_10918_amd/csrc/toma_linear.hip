@@ -244,8 +244,7 @@ static double epilogue_cost(const GemmPlan &p, const toma_linear_desc &d, int ro
 
 // 128 x 128 tiles, with four stages where every CU gets at most one
 static double medium_cost(int kind, const toma_linear_desc &d, int steps) {
-  const bool alone = (long long)((d.rows + 127) / 128) * ((d.N + 127) / 128) <= 256;
-  return rounds_cost(alone ? kAlone[kind] : kMedium[kind], d, steps);
+  return rounds_cost(medium_alone(d.rows, d.N) ? kAlone[kind] : kMedium[kind], d, steps);
 }
 
 // The fp32 partial sums of a K split are written and read once, by a kernel more.
@@ -309,6 +308,16 @@ static LinPlan plan_linear(const toma_linear_desc &d) {
 void plan_linear_tile(const toma_linear_desc &d, int32_t *out3) {
   const LinPlan p = plan_linear(d);
   out3[0] = p.bm; out3[1] = p.bn; out3[2] = p.nsplit;
+}
+
+const char *linear_kernel_name(const toma_linear_desc &d) {
+  const LinPlan p = plan_linear(d);
+  if (p.path == PATH_LARGE) return "large";
+  if (p.path == PATH_MEDIUM) return medium_alone(d.rows, d.N) ? "medium_four_stages" : "medium";
+  if (p.path == PATH_FEW) return "few_rows";
+  if (d.x_type == TOMA_MX8) return "small";
+  const int es = d.x_type == TOMA_F32 ? 4 : 2;
+  return gemm_async_fits(d.rows, d.N, gemm_steps(d.K, es), es) ? "planned" : "short";
 }
 
 template <typename T>

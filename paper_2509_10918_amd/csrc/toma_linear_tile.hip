@@ -313,8 +313,7 @@ static void go(const LinArgs &a, bool mx_out, hipStream_t st) {
 
 template <int KIND> static void pick(bool large, const LinArgs &a, bool mx_out, hipStream_t st) {
   if (large) return go<KIND, 256, 256, 2, 4, 2>(a, mx_out, st);
-  const long long wgs = (long long)((a.rows + 127) / 128) * ((a.N + 127) / 128);
-  if (wgs <= 256) return go<KIND, 128, 128, 2, 4, 4>(a, mx_out, st);
+  if (medium_alone(a.rows, a.N)) return go<KIND, 128, 128, 2, 4, 4>(a, mx_out, st);
   go<KIND, 128, 128, 2, 4, 2>(a, mx_out, st);
 }
 

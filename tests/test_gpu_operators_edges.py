@@ -7,7 +7,7 @@ import torch
 from paper_2509_10918_amd import binding as tb
 
 import operators_ref as ref
-from test_gpu_operators import DT, HALF, NAN, check_norm, gen, linear_case, randn, run_linear, within
+from test_gpu_operators import DT, HALF, NAN, check_linear, check_norm, gen, linear_case, randn, run_linear, within
 
 pytestmark = pytest.mark.gpu
 INF = float("inf")
@@ -43,6 +43,7 @@ def selecting_case(x_type, rows, K, N, lo, hi):
 SELECTING = [("bf16", 5, 64, 136), ("bf16", 3, 4096, 640), ("bf16", 200, 72, 136), ("bf16", 64, 4096, 256), ("bf16", 2000, 136, 2000), ("bf16", 4096, 640, 2560),
              ("bf16", 40, 24, 72), ("f32", 5, 64, 136), ("f32", 3, 8188, 260), ("f32", 947, 352, 1416), ("f32", 66, 4044, 136), ("f32", 40, 12, 72),
              ("mx8", 5, 64, 136), ("mx8", 77, 8192, 1280), ("mx8", 2000, 128, 2000), ("mx8", 1024, 1280, 5120), ("mx8", 4096, 640, 2560)]
+SELECTING += [("bf16", 8190, 64, 4096), ("mx8", 8190, 160, 4096), ("mx8", 2000, 288, 2000)]
 
 
 @pytest.mark.parametrize("act,lo,hi", [("gelu", -8.0, -3.0), ("gelu", -12.0, 3.0), ("gelu_tanh", -9.0, 3.0), ("silu", -80.0, 3.0)])
@@ -87,5 +88,23 @@ def test_logistic_gates_in_fp32(x_type, rows, K, N, act, lo, hi):
     y, _ = run_linear(x_type, x_type, x, w, None, None, act)
     u = 2 * (2 / torch.pi) ** 0.5 * (v + 0.044715 * v ** 3)
     within(y, want, want.abs() * 2.0 ** -24 * (5 + (5 * u.abs() if act == "gelu_tanh" else 0)) * (1 + 2.0 ** -10))
+
+
+# ---- every kernel by its name, over the number of its K steps ---------------------------------------------------------------------
+
+# (type, rows, N, kernel): K steps of 128 bytes a row, whole and with a part of the last
+STEPS = [("bf16", 2000, 2000, "medium_four_stages", range(1, 9)), ("mx8", 2000, 2000, "medium_four_stages", range(2, 9)), ("bf16", 3900, 2888, "medium", range(1, 6)),
+         ("mx8", 3900, 2888, "medium", range(1, 6)), ("bf16", 8190, 4096, "large", range(1, 5)), ("mx8", 8190, 4096, "large", range(1, 6)),
+         ("mx8", 300, 648, "small", range(1, 8))]
+STEPS = [(x, rows, K, N, kernel) for x, rows, N, kernel, steps in STEPS for n in steps
+         for K in ((64 * n, 64 * n + 40) if x == "bf16" else (128 * n, 128 * n + 32 * (1 + n % 3)))]
+
+
+@pytest.mark.parametrize("x_type,rows,K,N,kernel", STEPS)
+def test_every_number_of_K_steps(x_type, rows, K, N, kernel):
+    """The loads that a kernel counts on run ahead of its last steps, and its stages are reused in turn: few steps, and every remainder."""
+    y_type = "bf16" if x_type == "mx8" else x_type
+    assert tb.toma_profile_linear_kernel(tb.make_linear_desc(rows, K, N, x_type, y_type, "silu")) == kernel
+    check_linear(x_type, y_type, rows, K, N, "silu", True, False)
 
 

@@ -1,5 +1,5 @@
 """Host-side behaviour of the operators around the core modules, beyond their refusals: scratch sizes,
-and tensors of the right size in the wrong shape.  No GPU."""
+the choice of kernel, and tensors of the right size in the wrong shape.  No GPU."""
 import pytest
 import torch
 
@@ -16,6 +16,21 @@ def test_shapes_that_split_K_ask_for_the_scratch_of_their_partial_sums(x_type, r
     X, c = 1 << 20, (1 << 20 if x_type == "mx8" else None)   # an aligned address that no refused call reads
     call = lambda ws, n: tb.lib().toma_linear(tb._ref(d), X, c, X, c, None, None, X, None, ws, n, None)
     assert call(None, need) == 1 and call(X + 16, need) == 3 and call(X, 4 * split * rows * N - 1) == 4
+
+
+def test_kernels_by_name():
+    """The sizes at which the GPU tests try the activations' tails and values that are not finite reach every kernel, split and not."""
+    from test_gpu_operators_edges import SELECTING, STEPS
+    taken = set()
+    for x, rows, K, N in SELECTING:
+        d = tb.make_linear_desc(rows, K, N, x, "bf16" if x == "mx8" else x, "gelu")
+        taken.add((x, tb.toma_profile_linear_kernel(d), tb.toma_profile_linear(d)[2] > 1))
+    tiles = {(x, kernel, False) for x in ("bf16", "mx8") for kernel in ("medium", "medium_four_stages", "large")}
+    plain = {(x, kernel, split) for x in ("bf16", "f32") for kernel in ("few_rows", "planned") for split in (False, True)} | {(x, "short", False) for x in ("bf16", "f32")}
+    assert taken == tiles | plain | {("mx8", "small", False), ("mx8", "small", True)}
+    for x, rows, K, N, kernel in STEPS:
+        assert tb.toma_profile_linear_kernel(tb.make_linear_desc(rows, K, N, x, "bf16" if x == "mx8" else x, "silu")) == kernel, (x, rows, K, N)
+    assert tb.toma_profile_linear_kernel(tb.make_linear_desc(4, 12, 64, "bf16")) is None and tb.toma_profile_linear_kernel(None) is None
 
 
 # ---- tensors that hold as many elements in another order ------------------------------------------------------------------------
