@@ -108,3 +108,88 @@ def test_every_number_of_K_steps(x_type, rows, K, N, kernel):
     check_linear(x_type, y_type, rows, K, N, "silu", True, False)
 
 
+# ---- values that are not finite ---------------------------------------------------------------------------------------------
+
+def same_values(got, want):
+    """Equal, NaN where NaN."""
+    got, want = got.double(), want.double()
+    return torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(torch.nan_to_num(got), torch.nan_to_num(want))
+
+
+WHOLE_BLOCKS = [(x, rows, K, (N + 31) // 32 * 32) for x, rows, K, N in SELECTING]
+
+
+@pytest.mark.parametrize("x_type,rows,K,N", WHOLE_BLOCKS)
+def test_activations_of_infinities_and_nan(x_type, rows, K, N):
+    """Columns whose bias is infinite, NaN or huge: what the formula gives there, and every other column as without them.  The
+    formulas have -inf times zero at -inf (NaN); packed outputs hold no infinity (NaN), and a block's scale goes by its finite values."""
+    for act in ref.ACTS:
+        print(f"[not finite] {x_type} {rows} x {K} x {N} {act}", flush=True)
+        check_columns_that_are_not_finite(x_type, rows, K, N, act)
+
+
+def check_columns_that_are_not_finite(x_type, rows, K, N, act):
+    x, w, b, _, _, _ = linear_case(x_type, "", rows, K, N, act, True, False)
+    at = {3: INF, 8: -INF, 21: NAN, N - 1: INF, N // 2: 2.0 ** 120, N // 2 + 1: -2.0 ** 120}
+    odd = b.clone()
+    for n, v in at.items():
+        odd[n] = v
+    want = {n: NAN if v == -INF and act != "none" else (0.0 if v < 0 and act != "none" else v) for n, v in at.items()}
+    keep = [n for n in range(N) if n not in at]
+    for y_type in ("bf16", "mx8") if x_type == "mx8" else (x_type,):
+        y, s = run_linear(x_type, y_type, x, w, odd, None, act)
+        if y_type == "mx8":
+            y = ref.unpack(y, s)
+            full, _ = run_linear(x_type, "bf16", x, w, odd, None, act)
+            assert not s[:, N // 32:].any()
+            # the codes of the finite values; an output beside the rounding to bf16 may lie on the other side of a border
+            fin = torch.where(torch.isfinite(full), full.double(), torch.zeros_like(full, dtype=torch.float64))
+            code = s[:, :N // 32].long()
+            assert ((code >= ref.codes(fin * (1 - 2.0 ** -7))) & (code <= ref.codes(fin * (1 + 2.0 ** -7)))).all()
+            for n, v in want.items():
+                assert torch.isnan(y[:, n]).all() if v != v or v in (INF, -INF) else (y[:, n] == v).all(), (n, v)
+            sc = torch.exp2(code.double() - 127).repeat_interleave(32, 1)
+            within(y[:, keep], fin[:, keep], fin[:, keep].abs() * (2.0 ** -4 + 2.0 ** -7) + sc[:, keep] * 2.0 ** -10)
+            continue
+        plain, _ = run_linear(x_type, y_type, x, w, b, None, act)
+        assert torch.equal(y[:, keep], plain[:, keep])
+        for n, v in want.items():
+            assert same_values(y[:, n], torch.full_like(y[:, n], v)) or (v in (2.0 ** 120, -2.0 ** 120) and (y[:, n].double() / v - 1).abs().max() <= 2.0 ** -20), (n, v)
+
+
+@pytest.mark.parametrize("x_type,rows,K,N", WHOLE_BLOCKS)
+def test_a_row_that_is_not_finite(x_type, rows, K, N):
+    """One element of one row: all of that row and nothing else.  (8 bits: packing has made it NaN.)"""
+    for act in ref.ACTS:
+        for value in (INF, -INF, NAN):
+            print(f"[not finite row] {x_type} {rows} x {K} x {N} {act} {value}", flush=True)
+            check_row_that_is_not_finite(x_type, rows, K, N, value, act)
+
+
+def check_row_that_is_not_finite(x_type, rows, K, N, value, act):
+    g = gen(rows + K)
+    e = DT["f32" if x_type == "f32" else "bf16"]
+    xv, wv = randn(g, rows, K), randn(g, K, N) * K ** -0.5
+    wv[5] = 0.25 * (1 - 2 * (torch.arange(N, device="cuda") % 2))   # (no zeros in the row of weights that the value meets)
+    x0, w = xv.to(e), wv.to(e)
+    x1, bad = x0.clone(), rows // 2
+    x1[bad, 5] = value
+    if x_type == "mx8":
+        x0, x1, w = ref.pack(x0), ref.pack(x1), ref.pack(w.t().contiguous())
+        assert torch.isnan(ref.unpack(*x1)[bad, 5])
+        value = NAN
+    else:
+        x0, x1, w = (x0, None), (x1, None), (w, None)
+    keep = [r for r in range(rows) if r != bad]
+    pre = torch.full((N,), value, dtype=torch.float64, device="cuda") * (1 - 2 * (torch.arange(N, device="cuda") % 2))
+    want = torch.where(pre < 0, torch.full_like(pre, NAN), pre) if act != "none" else pre
+    for y_type in ("bf16", "mx8") if x_type == "mx8" else (x_type,):
+        y, s = run_linear(x_type, y_type, x1, w, None, None, act)
+        p, t = run_linear(x_type, y_type, x0, w, None, None, act)
+        assert torch.equal(y[keep], p[keep])
+        if y_type == "mx8":
+            assert torch.equal(s[keep], t[keep]) and torch.isnan(ref.unpack(y, s)[bad]).all() and not s[bad].any()
+        else:
+            assert same_values(y[bad], want)
+
+
