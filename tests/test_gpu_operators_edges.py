@@ -193,3 +193,63 @@ def check_row_that_is_not_finite(x_type, rows, K, N, value, act):
             assert same_values(y[bad], want)
 
 
+# ---- norm: accuracy of the row's statistic, and the end of its range ------------------------------------------------------------
+
+@pytest.mark.parametrize("rows,C,res,gain", [(205, 64, True, True), (37, 128, False, True), (130, 640, True, True), (65, 1280, False, False), (17, 4096, True, False),
+                                             (5, 8192, False, True), (3, 16384, True, True)])
+def test_norm_to_fp32_accuracy(rows, C, res, gain):
+    """x + r rounds once (u = 2^-24), which the sum of squares sees as 2 u; eight fused squares in fp32 add at most 8 u, the sums in
+    fp64 nothing; the inverse root halves these 10 u, rounds once itself, and two products round: u + 5 u + u + 2 u."""
+    print(f"[norm fp32] {rows} x {C} residual={res} gain={gain}", flush=True)
+    g = gen(rows * 3 + C)
+    x = randn(g, rows, C) * torch.exp2(torch.randint(-20, 21, (rows, 1), generator=g, device="cuda").float())
+    r = randn(g, rows, C) if res else None
+    gamma = 1 + 0.3 * randn(g, C) if gain else None
+    y = torch.empty_like(x)
+    tb.toma_rmsnorm(tb.make_norm_desc(rows, C, 1e-6, "f32"), x, r, gamma, None, y)
+    _, want = ref.norm(x, r, gamma, float(torch.tensor(1e-6, dtype=torch.float32)))
+    within(y, want, want.abs() * 9 * 2.0 ** -24 * (1 + 2.0 ** -10) + 2.0 ** -149)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("C", [64, 1280, 8192])
+@pytest.mark.parametrize("value", [2.0 ** 64, -2.0 ** 100])
+def test_norm_of_a_row_whose_squares_leave_the_range(dtype, C, value):
+    """Zeros in that row, plain and packed (codes 0), h as it is; the other rows as ever.  A row of 2^61 is still in the range."""
+    g = gen(C)
+    x = randn(g, 5, C).to(DT[dtype])
+    x[3] = 2.0 ** 61
+    x[1, 7] = value
+    r = torch.zeros_like(x)
+    d = {out: tb.make_norm_desc(5, C, 1e-6, dtype, out or dtype) for out in ("", "mx8")}
+    h, y = torch.empty_like(x), torch.empty_like(x)
+    tb.toma_rmsnorm(d[""], x, r, None, h, y)
+    assert torch.equal(h, x) and not y[1].any()
+    q, s = tb.alloc_mx(5, C)
+    tb.toma_rmsnorm(d["mx8"], x, r, None, h, q.fill_(0x55), s.fill_(0x55))
+    assert torch.equal(h, x) and not (q[1] & 0x7f).any() and not s[1].any()
+    keep = [0, 2, 3, 4]
+    check_norm(x[keep], None, None, 1e-6, "")
+    check_norm(x[keep], None, None, 1e-6, "mx8")
+    want = torch.empty_like(x[keep])
+    tb.toma_rmsnorm(tb.make_norm_desc(4, C, 1e-6, dtype), x[keep], r[keep], None, None, want)
+    assert torch.equal(y[keep], want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("value", [INF, -INF, NAN])
+def test_norm_of_a_row_that_is_not_finite(dtype, value):
+    """The formula's result: an infinity makes its own element NaN and the others zero, NaN makes the row NaN."""
+    g = gen(4)
+    x = randn(g, 6, 96).to(DT[dtype])
+    x[2, 50] = value
+    y, q, s = torch.empty_like(x), *tb.alloc_mx(6, 96)
+    tb.toma_rmsnorm(tb.make_norm_desc(6, 96, 1e-6, dtype), x, None, None, None, y)
+    tb.toma_rmsnorm(tb.make_norm_desc(6, 96, 1e-6, dtype, "mx8"), x, None, None, None, q, s)
+    nan = torch.zeros(6, 96, dtype=torch.bool, device="cuda")
+    nan[2, 50 if value == value else slice(None)] = True
+    for v in (y.double(), ref.unpack(q, s)):
+        assert torch.equal(torch.isnan(v), nan) and not torch.nan_to_num(v[2]).any()
+    check_norm(x[[0, 1, 3, 4, 5]], None, None, 1e-6, "")
+
+
