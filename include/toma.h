@@ -290,8 +290,8 @@ int toma_mlp(int32_t dtype, int32_t rows, int32_t C, int32_t hidden, const void 
  *   toma_mx_quantize         X [rows, K] (x_type TOMA_F32 / TOMA_BF16) -> Q, S
  *   toma_mx_quantize_weight  W [K, N] (w_type) -> Q [N, K], S [N, stride]: the layout in which a product takes its
  *                            weights, blocks of 32 input channels of one output channel; once per weight
- *   toma_mx_dequantize       Q, S -> Y [rows, K] in y_type: the values they stand for (bf16 holds all of them exactly, but
- *                            for magnitudes below 2^-126)
+ *   toma_mx_dequantize       Q, S -> Y [rows, K] in y_type: the values they stand for, exactly below 2^128 (bf16: from 2^-126 on, smaller
+ *                            ones rounded).  A magnitude of 1.9375 * 2^127 or more packs as 2^128 and comes back as an infinity
  * Limits: K <= 2^20, rows * max(K, 128) < 2^34; weights: K * N < 2^31.
  */
 size_t toma_mx_scale_stride(int32_t K); /* 4 ceil(K / 128); 0 when K is not a positive multiple of 32 */

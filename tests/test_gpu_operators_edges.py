@@ -253,3 +253,30 @@ def test_norm_of_a_row_that_is_not_finite(dtype, value):
     check_norm(x[[0, 1, 3, 4, 5]], None, None, 1e-6, "")
 
 
+# ---- packing at the ends of the range ---------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_unpacking_the_ends_of_the_range(dtype):
+    """Packed values are exact in fp32 and bf16 between 2^-126 and 2^128; a packed 2^128 itself (a magnitude of at
+    least 1.9375 x 2^127 rounds to it) is an infinity in either."""
+    x = torch.zeros(8, 64, device="cuda")
+    x[0, 0] = torch.finfo(DT[dtype]).max
+    x[1, 0], x[1, 1] = -torch.finfo(DT[dtype]).max, 1.0
+    x[2, 0] = 1.921875 * 2.0 ** 127        # below the border: 1.875 x 2^127
+    x[3, 0], x[3, 1] = 2.0 ** 127, -2.0 ** 118
+    x[4, 0], x[4, 33] = 2.0 ** -126, 2.0 ** -120
+    x[5, 0], x[5, 1] = 448 * 2.0 ** -127, 2.0 ** -126
+    x[6, 0] = 2.0 ** -133
+    x[7, 0] = 1.0
+    x = x.to(DT[dtype])
+    q, s = tb.alloc_mx(8, 64)
+    tb.toma_mx_quantize(x, q, s)
+    want = ref.unpack(q, s)
+    assert want[0, 0] == 2.0 ** 128 and want[1, 0] == -2.0 ** 128 and want[2, 0] == 1.875 * 2.0 ** 127
+    for out in ("f32", "bf16"):
+        y = torch.empty(8, 64, dtype=DT[out], device="cuda")
+        tb.toma_mx_dequantize(q, s, y)
+        assert y[0, 0] == INF and y[1, 0] == -INF
+        y, v = y.double(), want.clone()
+        y[0, 0], y[1, 0], v[0, 0], v[1, 0] = 0, 0, 0, 0
+        assert torch.equal(y, v)
