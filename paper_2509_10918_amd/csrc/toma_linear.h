@@ -108,12 +108,10 @@ __device__ __forceinline__ bf16x8 bf16_half(const i32x8 &v, int e) {
   const i32x4 h = e ? __builtin_shufflevector(v, v, 4, 5, 6, 7) : __builtin_shufflevector(v, v, 0, 1, 2, 3);
   return __builtin_bit_cast(bf16x8, h);
 }
-// byte g of d[0 .. n - 1] (masked) as the bytes of one word
-__device__ __forceinline__ uint32_t gather_bytes(const uint32_t *d, int n, uint32_t mask, int g) {
+// byte g of d[0] and of d[1] (masked) as the low bytes of a word
+__device__ __forceinline__ uint32_t gather_bytes(const uint32_t (&d)[2], uint32_t mask, int g) {
   const uint32_t sel = (uint32_t)g | (uint32_t)(4 + g) << 8;  // byte g of the second, then of the first operand
-  const uint32_t lo = __builtin_amdgcn_perm(n > 1 ? d[1] & mask : 0u, d[0] & mask, sel);
-  const uint32_t hi = n > 2 ? __builtin_amdgcn_perm(n > 3 ? d[3] & mask : 0u, d[2] & mask, sel) : 0u;
-  return (lo & 0xffffu) | hi << 16;
+  return __builtin_amdgcn_perm(d[1] & mask, d[0] & mask, sel) & 0xffffu;
 }
 // Turns a 4 x 4 matrix of bytes over between a word's bytes and the four lane groups: byte b of the result is byte g of the word
 // of lane group b (same lane of the group).  Halves of the wave first: a word's two bytes for either group of the half, from

@@ -19,18 +19,19 @@ __device__ __forceinline__ void buffer_to_lds_pair(const uint8_t *base, uint32_t
                "v"(off[0]), "v"(off[1]), "s"(rsrc) : "memory", "m0");
 }
 
+constexpr int kSmall = 64, kSmallWaves = 4;  // rows and columns of a tile; two by two waves
+
 // RAGGED: K is no multiple of a step
-template <int BM, int BN, int WM, int WN, int UNITS, bool MX_OUT, bool RAGGED>
-__global__ __launch_bounds__(64 * WM * WN) void k_linear_small(const LinArgs a, int tiles_m, int tiles_n, int nsplit, float *part) {
-  constexpr int NW = WM * WN, WTM = BM / WM, WTN = BN / WN, TM = WTM / 16, TN = WTN / 16;
-  constexpr int BK = 128;
+template <bool MX_OUT, bool RAGGED>
+__global__ __launch_bounds__(64 * kSmallWaves) void k_linear_small(const LinArgs a, int tiles_m, int tiles_n, int nsplit, float *part) {
+  constexpr int BM = kSmall, BN = kSmall, NW = kSmallWaves, WN = 2, WTM = BM / 2, WTN = BN / 2, TM = 2, TN = 2;
+  constexpr int BK = 128, UNITS = 2;
   constexpr int NIA = BM / 8 / NW, NIB = BN / 8 / NW;  // load instructions (1 KiB) per wave and step
-  constexpr int NS = (BM + BN) / 16, NIS = (NS + 2 * NW - 1) / (2 * NW);  // per unit: half of four steps' scale codes
-  constexpr int L = 2 * (NIA + NIB) + NIS;             // loads per wave and unit
+  constexpr int L = 2 * (NIA + NIB) + 1;               // loads per wave and unit: with half of four steps' scale codes
   constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, S_BYTES = (BM + BN) * 16;
-  constexpr int SLOTS = (UNITS + 3) / 2;               // of four steps' codes
+  constexpr int SLOTS = 2;                             // of four steps' codes
   constexpr int B_AT = UNITS * 2 * A_BYTES, S_AT = B_AT + UNITS * 2 * B_BYTES, LDS_BYTES = S_AT + SLOTS * S_BYTES;
-  static_assert(TM % 2 == 0 && TM <= 4 && TN <= 4 && (UNITS - 1) * L < 64, "blocks spelled out below; the wait count's range");
+  static_assert(NIA == 2 && NIB == 2 && (BM + BN) / 16 == 2 * NW, "loads in pairs; one load of scale codes per wave and unit");
   static_assert(NW * kEpilogueFloats<TN> * 4 <= LDS_BYTES, "the epilogue's rows fit the stages");
   __shared__ __align__(1024) uint8_t lds[LDS_BYTES];
 
@@ -66,17 +67,14 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_small(const LinArgs a, 
   const uint32_t l0 = lds_addr_of(lds);
   const uint32_t lx = l0 + (uint32_t)(w * NIA * 1024), lw = l0 + B_AT + (uint32_t)(w * NIB * 1024);
   auto issue_codes = [&](int chunk, int part) {  // half of the rows' codes of four steps; behind the end of a row its last repeat
-#pragma unroll
-    for (int t = 0; t < NIS; t++) {
-      const int sr = ((part * NW + w) * NIS + t) % NS * 16;
-      const bool of_x = sr < BM;
-      const uint8_t *base = of_x ? a.Xs + (size_t)m0 * a.xs_stride : a.Ws + (size_t)n0 * a.xs_stride;
-      const int row = min(sr + (lane >> 2) - (of_x ? 0 : BM), of_x ? a.rows - 1 - m0 : a.N - 1 - n0);
-      const uint32_t off = (uint32_t)row * (uint32_t)a.xs_stride + (uint32_t)min(16 * chunk + 4 * (lane & 3), a.xs_stride - 4);
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(l0 + S_AT + (uint32_t)(__builtin_amdgcn_readfirstlane(chunk % SLOTS) * S_BYTES + sr * 16)),
-                   "v"(off), "s"(base)
-                   : "memory", "m0");
-    }
+    const int sr = (part * NW + w) * 16;
+    const bool of_x = sr < BM;
+    const uint8_t *base = of_x ? a.Xs + (size_t)m0 * a.xs_stride : a.Ws + (size_t)n0 * a.xs_stride;
+    const int row = min(sr + (lane >> 2) - (of_x ? 0 : BM), of_x ? a.rows - 1 - m0 : a.N - 1 - n0);
+    const uint32_t off = (uint32_t)row * (uint32_t)a.xs_stride + (uint32_t)min(16 * chunk + 4 * (lane & 3), a.xs_stride - 4);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(l0 + S_AT + (uint32_t)(__builtin_amdgcn_readfirstlane(chunk % SLOTS) * S_BYTES + sr * 16)),
+                 "v"(off), "s"(base)
+                 : "memory", "m0");
   };
   auto issue = [&](int slot, int u) {
     issue_codes(((u - 1) >> 1) + 1, (u - 1) & 1);  // (a chunk is complete with its first unit's loads)
@@ -136,8 +134,8 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_small(const LinArgs a, 
       for (int i = 0; i < TM; i++) dx[i] = raw_x[i][h];
 #pragma unroll
       for (int i = 0; i < TN; i++) dw[i] = raw_w[i][h];
-      cx[h] = gather_bytes(dx, TM, mask, g);
-      cw[h] = gather_bytes(dw, TN, mask, g);
+      cx[h] = gather_bytes(dx, mask, g);
+      cw[h] = gather_bytes(dw, mask, g);
     }
   };
 
@@ -169,19 +167,11 @@ __global__ __launch_bounds__(64 * WM * WN) void k_linear_small(const LinArgs a, 
     read(integral_constant<int, set ^ 1>(), next, u + 1);
     issue(slot, u + UNITS);
     __builtin_amdgcn_sched_barrier(0);
-    auto row = [&](auto h_, auto i_) {
-      constexpr int h = decltype(h_)::value, i = decltype(i_)::value;
-      auto one = [&](auto j_) {
-        constexpr int j = decltype(j_)::value;
-        if constexpr (i < TM && j < TN)
-          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[set][h][j], fx[set][h][i], acc[i][j], 0, 0, j, (int)cw[h], i, (int)cx[h]);
-      };
-      one(integral_constant<int, 0>()); one(integral_constant<int, 1>()); one(integral_constant<int, 2>()); one(integral_constant<int, 3>());
+    auto one = [&](auto h_, auto i_, auto j_) {
+      constexpr int h = decltype(h_)::value, i = decltype(i_)::value, j = decltype(j_)::value;
+      acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[set][h][j], fx[set][h][i], acc[i][j], 0, 0, j, (int)cw[h], i, (int)cx[h]);
     };
-    auto half = [&](auto h_) {
-      row(h_, integral_constant<int, 0>()); row(h_, integral_constant<int, 1>());
-      row(h_, integral_constant<int, 2>()); row(h_, integral_constant<int, 3>());
-    };
+    auto half = [&](auto h_) { one(h_, even, even); one(h_, even, odd); one(h_, odd, even); one(h_, odd, odd); };
     half(even);
     half(odd);
     __builtin_amdgcn_sched_barrier(0);
@@ -246,12 +236,11 @@ __global__ __launch_bounds__(256) void k_linear_finish(const LinArgs a, int nspl
   }
 }
 
-template <int BM, int BN, int WM, int WN, int UNITS>
-static void go(const LinArgs &a, bool mx_out, int nsplit, float *part, hipStream_t st) {
-  const int tm = (a.rows + BM - 1) / BM, tn = (a.N + BN - 1) / BN;
-  const dim3 grid((unsigned)(tm * (long long)tn), (unsigned)nsplit), block(64 * WM * WN);
+void launch_linear_small(const LinArgs &a, bool mx_out, int nsplit, float *part, hipStream_t st) {
+  const int tm = (a.rows + kSmall - 1) / kSmall, tn = (a.N + kSmall - 1) / kSmall;
+  const dim3 grid((unsigned)(tm * (long long)tn), (unsigned)nsplit), block(64 * kSmallWaves);
   auto run = [&](auto out, auto ragged) {
-    hipLaunchKernelGGL((k_linear_small<BM, BN, WM, WN, UNITS, decltype(out)::value, decltype(ragged)::value>), grid, block, 0, st, a, tm, tn, nsplit,
+    hipLaunchKernelGGL((k_linear_small<decltype(out)::value, decltype(ragged)::value>), grid, block, 0, st, a, tm, tn, nsplit,
                        nsplit > 1 ? part : nullptr);
   };
   const bool ragged = a.K % 128 != 0;
@@ -263,10 +252,6 @@ static void go(const LinArgs &a, bool mx_out, int nsplit, float *part, hipStream
     if (mx_out) hipLaunchKernelGGL(k_linear_finish<true>, blocks, dim3(256), 0, st, a, nsplit, part, per_row);
     else hipLaunchKernelGGL(k_linear_finish<false>, blocks, dim3(256), 0, st, a, nsplit, part, per_row);
   }
-}
-
-void launch_linear_small(const LinArgs &a, bool mx_out, int nsplit, float *part, hipStream_t st) {
-  go<64, 64, 2, 2, 2>(a, mx_out, nsplit, part, st);
 }
 
 }  // namespace toma
