@@ -7,7 +7,7 @@ import torch
 from paper_2509_10918_amd import binding as tb
 
 import operators_ref as ref
-from test_gpu_operators import DT, HALF, NAN, check_linear, check_norm, gen, linear_case, randn, run_linear, within
+from test_gpu_operators import DT, HALF, NAN, check_linear, check_norm, ffn_call, ffn_inputs, gen, linear_case, randn, run_linear, within
 
 pytestmark = pytest.mark.gpu
 INF = float("inf")
@@ -280,3 +280,109 @@ def test_unpacking_the_ends_of_the_range(dtype):
         y, v = y.double(), want.clone()
         y[0, 0], y[1, 0], v[0, 0], v[1, 0] = 0, 0, 0, 0
         assert torch.equal(y, v)
+
+
+# ---- 8-bit products at the ends of the scales --------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("x_type,rows,K,N", [c for c in SELECTING if c[0] == "mx8"])
+def test_products_of_extreme_scales(x_type, rows, K, N):
+    """Every scale code from 0 to 254 on either side, chosen block by block so that the scales nearly cancel in the products."""
+    g = gen(rows + K + 2 * N)
+
+    def elements(*shape):
+        return torch.randint(-64, 65, shape, generator=g, device="cuda").float().to(torch.float8_e4m3fn).view(torch.uint8)
+
+    blocks = K // 32
+    c = torch.linspace(0, 254, blocks, device="cuda").round().long()[torch.randperm(blocks, generator=g, device="cuda")]
+    c[0], c[-1] = 0, 254
+
+    def codes(n, base):
+        s = torch.randint(0, 256, (n, ref.stride(K)), generator=g, device="cuda")   # (whatever stands behind the row's blocks)
+        s[:, :blocks] = (base + torch.randint(-2, 3, (n, blocks), generator=g, device="cuda")).clamp(0, 254)
+        return s.to(torch.uint8)
+
+    x, w = (elements(rows, K), codes(rows, c)), (elements(N, K), codes(N, 254 - c))
+    y, _ = run_linear("mx8", "bf16", x, w, None, None, "none")
+    x64, w64 = ref.unpack(*x), ref.unpack(*w).t().contiguous()
+    want, size = x64 @ w64, x64.abs() @ w64.abs()
+    tol = size * (K * 2.0 ** -24 + 2.0 ** -12) + 2.0 ** -20 * want.abs()
+    within(y, want, (want.abs() + tol) * HALF[torch.bfloat16] + tol)
+
+
+# ---- one tensor in two places, and calls that a graph repeats ------------------------------------------------------------------------
+
+@pytest.mark.parametrize("out", ["", "mx8"])
+@pytest.mark.parametrize("C", [64, 640, 8192])
+def test_norm_of_a_tensor_with_itself(out, C):
+    """x as its own residual, and the sum stored over it: as with tensors of their own."""
+    x = randn(gen(C), 70, C).to(torch.bfloat16)
+    d = tb.make_norm_desc(70, C, 1e-6, "bf16", out or "bf16")
+    results = []
+    for alias in (False, True):
+        a, r = x.clone(), x.clone()
+        h = torch.empty_like(x)
+        if alias:
+            r = h = a
+        y = tb.alloc_mx(70, C) if out else (torch.empty_like(x), None)
+        tb.toma_rmsnorm(d, a, r, None, h, *y)
+        results.append((h, *(y if out else y[:1])))
+    assert torch.equal(results[0][0], 2 * x)
+    assert all(torch.equal(p, q) for p, q in zip(*results))
+
+
+@pytest.mark.parametrize("x_type", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [1, 40, 700, 4096])
+def test_linear_with_its_input_as_residual(x_type, rows):
+    x, w, b, _, _, _ = linear_case(x_type, x_type, rows, 640, 640, "silu", True, False)
+    d = tb.make_linear_desc(rows, 640, 640, x_type, None, "silu")
+    ws, y, want = tb.alloc_linear_workspace(d), torch.empty_like(x[0]), torch.empty_like(x[0])
+    tb.toma_linear(d, x[0], None, w[0], None, b, x[0].clone(), want, None, ws)
+    tb.toma_linear(d, x[0], None, w[0], None, b, x[0], y, None, ws)
+    assert torch.equal(y, want)
+
+
+@pytest.mark.parametrize("x_type,w_type", [("bf16", "bf16"), ("bf16", "mx8"), ("f32", "f32")])
+@pytest.mark.parametrize("rows", [3, 130, 1500])
+def test_ffn_over_either_of_its_inputs(x_type, w_type, rows):
+    """Y is X, R, or both of them in one tensor."""
+    t = ffn_inputs(rows, 320, 640, x_type, w_type, True, True)
+    d = tb.make_ffn_desc(rows, 320, 640, 1e-6, x_type, w_type, "gelu")
+    ws = tb.alloc_ffn_workspace(d)
+    for same in (False, True):
+        base = dict(t, R=t["X"]) if same else t
+        want = torch.empty_like(t["X"])
+        ffn_call(base, d, want, ws)
+        for over in ("X", "R"):
+            now = dict(base, X=base["X"].clone(), R=base["R"].clone())
+            if same:
+                now["R"] = now["X"]
+            ffn_call(now, d, now[over], ws)
+            assert torch.equal(now[over], want), (same, over)
+
+
+def test_packing_and_product_replayed_from_a_graph():
+    """Packing, an 8-bit product with packed output and its unpacking in one graph, replayed on new inputs between eager calls."""
+    rows, K, N = 77, 2080, 640
+    x = randn(gen(1), rows, K).to(torch.bfloat16)
+    w = tb.alloc_mx(N, K)
+    tb.toma_mx_quantize_weight(randn(gen(2), K, N).to(torch.bfloat16), *w)
+    d = tb.make_linear_desc(rows, K, N, "mx8", "mx8", "gelu")
+    buffers = [(tb.alloc_mx(rows, K), tb.alloc_mx(rows, N), torch.empty(rows, N, device="cuda"), tb.alloc_linear_workspace(d)) for _ in range(2)]
+
+    def call(q, p, y, ws):
+        tb.toma_mx_quantize(x, *q)
+        tb.toma_linear(d, *q, *w, None, None, *p, ws)
+        tb.toma_mx_dequantize(*p, y)
+
+    call(*buffers[0])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(*buffers[0])
+    for k in range(4):
+        x.copy_(randn(gen(10 + k), rows, K))
+        call(*buffers[1])
+        buffers[0][2].zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(buffers[0][2], buffers[1][2]) and buffers[0][2].any(), k
