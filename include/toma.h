@@ -311,7 +311,8 @@ int toma_mx_dequantize(int32_t y_type, int32_t rows, int32_t K, const void *Q, c
  *   Y        out  [rows, C]       y_type; with TOMA_MX8 the elements, and Ys_opt the scale codes; overlaps no input
  * Limits: C % 32 == 0, C <= 16384, rows * max(C, 64) < 2^34; x_type TOMA_F32 / TOMA_BF16; y_type x_type or TOMA_MX8 (Ys_opt
  * is non-NULL exactly then).
- * Rows may be heads: the norm of 64-wide queries and keys is a call with C = 64 and rows = tokens * heads.
+ * Rows may be heads: the norm of 64-wide queries and keys is a call with C = 64 and rows = tokens * heads (for attention of the
+ * caller's own: toma_attend forms its queries and keys inside).
  */
 typedef struct {
   int32_t rows, C;
@@ -330,7 +331,8 @@ int toma_rmsnorm(const toma_norm_desc *desc, const void *X, const void *R_opt, c
  *   bias_opt  in   [N]         fp32 products: fp32; else bf16
  *   R_opt     in   [rows, N]   as bias; may be Y itself
  *   Y         out  [rows, N]   y_type (TOMA_MX8: elements, Ys_opt their scale codes); overlaps no other input
- * Products accumulate in fp32, the epilogue is evaluated in fp32 and rounded once.  For bf16 and packed outputs TOMA_ACT_GELU is a
+ * Products accumulate in fp32 (TOMA_MX8: the matrix instruction aligns the 128 products of a step to the largest before it adds them,
+ * which costs up to 2^-12 of that), the epilogue is evaluated in fp32 and rounded once.  For bf16 and packed outputs TOMA_ACT_GELU is a
  * fit in fp32, off by at most 2^-14 of its value (toma_mlp's takes the error function); -inf gives NaN, as the formulas do.
  * Types: x_type TOMA_F32 / TOMA_BF16 with y_type the same; x_type TOMA_MX8 with y_type TOMA_BF16 or TOMA_MX8.
  * Limits: TOMA_F32: K % 4 == 0, N % 4 == 0; TOMA_BF16: K % 8 == 0, N % 8 == 0; TOMA_MX8: K % 32 == 0 and N % 8 == 0 (y_type

@@ -202,6 +202,7 @@ static GemmPlan plan_tiles(int rows, int N, int K_steps, int elem_size) {
 // Estimated times in microseconds, fitted to measurements of every kernel on the same shapes (replayed graphs, so without host
 // time).  A kernel's workgroups run in rounds of what the chip holds; a round costs a fixed part (first loads, epilogue) and a part
 // per K step of 128 bytes a row, which is smaller where CUs are left over or hold one workgroup instead of two.
+// The estimates are off by up to a quarter, so between kernels closer than that the choice may miss the faster one.
 // Measured and estimated, us (bf16, rows x K x N):            large        medium       planned tiles
 //   16384 x 4096 x 8192                                       795 / 775    984 / 899    1003 / 965
 //   4096 x 640 x 2560                                         21.1 / 23.0  20.4 / 22.2  28.9 / 32.7
