@@ -5,6 +5,8 @@ hands raw pointers to the library and raises TomaError on a non-zero status.  Th
 path: if libtoma.so has not been built, loading it fails.
 """
 import ctypes
+import functools
+import math
 import os
 
 import torch
@@ -271,33 +273,38 @@ _TORCH = {TOMA_F32: torch.float32, TOMA_BF16: torch.bfloat16, TOMA_MX8: torch.ui
 _ROWS, _WEIGHT, _CODES = range(3)   # what a tensor is
 
 
-def _whole_rows(shape, width, several):
-    """Whether a contiguous tensor of this shape is rows of `width` one after the other: its last dimensions are one row, it is flat, or
-    (several) its last dimension is more than one row: the norm of single heads."""
+@functools.lru_cache(maxsize=1024)
+def _fits(shape, want, kind):
+    """Whether a contiguous tensor of this shape holds what one of the shape `want` ((rows, width), (width,)) does.  Weights: any whose last
+    dimension is right.  Rows: one after the other, so that the last dimensions are one row, or all of it is flat, or (not of codes) the
+    last dimension is several: the norm of single heads."""
+    if math.prod(shape) != math.prod(want):
+        return False
+    width = want[-1]
+    if len(want) == 1 or len(shape) == 1 or shape[-1] == width:
+        return kind != _WEIGHT or shape[-1] == width
+    if kind == _WEIGHT:
+        return False
     n = 1
     for s in reversed(shape):
         n *= s
         if n == width:
             return True
-    return len(shape) == 1 or (several and len(shape) > 0 and shape[-1] % width == 0)
+    return kind == _ROWS and len(shape) > 0 and shape[-1] % width == 0
 
 
-def _check_layout(what, t, dtype, shape, kind, device):
-    """For a tensor that is not exactly of the expected shape, type and device: refuses it, unless it is the same rows under another
-    shape (weights: any whose last dimension is right)."""
-    count = 1
-    for n in shape:
-        count *= n
-    if kind == _WEIGHT and t.shape[-1:] != shape[-1:]:
-        raise ValueError(f"{what}: last dimension {shape[-1]} expected, got the shape {tuple(t.shape)}")
+def _refuse(what, t, dtype, shape, kind, device):
+    """The reason why a tensor is not taken."""
+    count, got = math.prod(shape), tuple(t.shape)
+    if kind == _WEIGHT and got[-1:] != shape[-1:]:
+        raise ValueError(f"{what}: last dimension {shape[-1]} expected, got the shape {got}")
     if t.dtype is not dtype or t.numel() != count:
         raise ValueError(f"{what}: {count} elements of {dtype} expected, got {t.numel()} of {t.dtype}")
-    if len(shape) > 1 and not _whole_rows(t.shape, shape[-1], kind == _ROWS):
-        raise ValueError(f"{what}: rows of {shape[-1]} expected, got the shape {tuple(t.shape)}")
+    if not _fits(got, shape, kind):
+        raise ValueError(f"{what}: rows of {shape[-1]} expected, got the shape {got}")
     if t.get_device() < 0 or not t.is_contiguous():
         raise ValueError(f"{what}: libtoma takes contiguous CUDA tensors")
-    if t.get_device() != device:
-        raise ValueError(f"{what} lies on {t.device}, the current device is cuda:{device}")
+    raise ValueError(f"{what} lies on {t.device}, the current device is cuda:{device}")
 
 
 class _Call:
@@ -307,23 +314,23 @@ class _Call:
     __slots__ = ("device",)
 
     def __init__(self):
-        self.device = torch.cuda.current_device() if torch.cuda.is_initialized() else 0
+        self.device = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else 0
 
-    def arg(self, what, t, code, shape, kind=_ROWS):
+    def arg(self, what, t, dtype, shape, kind=_ROWS):
         """shape: (rows, width) or (width,)"""
         if t is None:
             return None
-        dtype = _TORCH.get(code)
-        if t.shape != shape or t.dtype is not dtype or t.get_device() != self.device or not t.is_contiguous():
-            _check_layout(what, t, dtype, shape, kind, self.device)
+        s = t.shape
+        if (s != shape and not _fits(s, shape, kind)) or t.dtype is not dtype or t.get_device() != self.device or not t.is_contiguous():
+            _refuse(what, t, dtype, shape, kind, self.device)
         return t.data_ptr()
 
     def codes(self, what, t, rows, width):
-        return self.arg(what, t, TOMA_MX8, (rows, _scale_stride(width)), _CODES)
+        return None if t is None else self.arg(what, t, torch.uint8, (rows, _scale_stride(width)), _CODES)
 
     def scratch(self, ws):
         """Pointer and bytes of a scratch tensor (None: no scratch)."""
-        return (None, 0) if ws is None else (self.arg("ws", ws, TOMA_MX8, (ws.numel(),)), ws.numel())
+        return (None, 0) if ws is None else (self.arg("ws", ws, torch.uint8, (ws.numel(),)), ws.numel())
 
     def stream(self):
         return torch._C._cuda_getCurrentRawStream(self.device)
@@ -348,8 +355,8 @@ def alloc_mx(rows, K, device="cuda"):
 
 def _pack_call(name, what, plain, shape, code, lead, rows, K, Q, S):
     c = _Call()
-    p = c.arg(what, plain, max(code, 0), shape)
-    q, s = c.arg("Q", Q, TOMA_MX8, (rows, K)), c.codes("S", S, rows, K)
+    p = c.arg(what, plain, _TORCH[max(code, 0)], shape)
+    q, s = c.arg("Q", Q, torch.uint8, (rows, K)), c.codes("S", S, rows, K)
     args = (q, s, p) if what == "Y" else (p, q, s)
     _check(getattr(lib(), name)(code, *lead, *args, c.stream()), name)
 
@@ -378,10 +385,11 @@ def make_norm_desc(rows, C, eps, x_type, y_type=None):
 
 def toma_rmsnorm(desc, X, R, gamma, H, Y, Ys=None):
     """X, R, H, Y: rows of C, under any leading dimensions (or several rows in the last: heads)."""
-    rows, C, x = desc.rows, desc.C, desc.x_type
-    n, c = (rows, C), _Call()
-    _check(lib().toma_rmsnorm(_ref(desc), c.arg("X", X, x, n), c.arg("R", R, x, n), c.arg("gamma", gamma, x, (C,)), c.arg("H", H, x, n),
-                              c.arg("Y", Y, desc.y_type, n), c.codes("Ys", Ys, rows, C), c.stream()),
+    rows, C, x, y = desc.rows, desc.C, desc.x_type, desc.y_type
+    e, n, c = _TORCH.get(x), (rows, C), _Call()
+    arg = c.arg
+    _check(lib().toma_rmsnorm(_ref(desc), arg("X", X, e, n), arg("R", R, e, n), arg("gamma", gamma, e, (C,)), arg("H", H, e, n),
+                              arg("Y", Y, e if y == x else _TORCH.get(y), n), c.codes("Ys", Ys, rows, C), c.stream()),
            "toma_rmsnorm")
 
 
@@ -404,12 +412,12 @@ def alloc_linear_workspace(desc, device="cuda"):
 
 def toma_linear(desc, X, Xs, W, Ws, bias, R, Y, Ys, ws):
     rows, K, N, x = desc.rows, desc.K, desc.N, desc.x_type
-    e = TOMA_F32 if x == TOMA_F32 else TOMA_BF16   # bias and residual
+    t, e, n = _TORCH.get(x), torch.float32 if x == TOMA_F32 else torch.bfloat16, (rows, N)   # e: type of bias and residual
     c = _Call()
-    w = c.arg("W", W, x, (N, K) if x == TOMA_MX8 else (K, N), _WEIGHT)
-    _check(lib().toma_linear(_ref(desc), c.arg("X", X, x, (rows, K)), c.codes("Xs", Xs, rows, K), w,
-                             c.codes("Ws", Ws, N, K), c.arg("bias", bias, e, (N,)), c.arg("R", R, e, (rows, N)),
-                             c.arg("Y", Y, desc.y_type, (rows, N)), c.codes("Ys", Ys, rows, N), *c.scratch(ws), c.stream()),
+    arg, codes = c.arg, c.codes
+    w = arg("W", W, t, (N, K) if x == TOMA_MX8 else (K, N), _WEIGHT)
+    _check(lib().toma_linear(_ref(desc), arg("X", X, t, (rows, K)), codes("Xs", Xs, rows, K), w, codes("Ws", Ws, N, K), arg("bias", bias, e, (N,)),
+                             arg("R", R, e, n), arg("Y", Y, _TORCH.get(desc.y_type), n), codes("Ys", Ys, rows, N), *c.scratch(ws), c.stream()),
            "toma_linear")
 
 
@@ -429,13 +437,14 @@ def alloc_ffn_workspace(desc, device="cuda"):
 
 
 def toma_ffn(desc, X, R, gamma, W1, W1s, b1, W2, W2s, b2, Y, ws):
-    C, hidden, x, w = desc.C, desc.hidden, desc.x_type, desc.w_type
-    n, c = (desc.rows, C), _Call()
+    C, hidden, w = desc.C, desc.hidden, desc.w_type
+    e, t, n, c = _TORCH.get(desc.x_type), _TORCH.get(w), (desc.rows, C), _Call()
+    arg, codes = c.arg, c.codes
     up, down = ((hidden, C), (C, hidden)) if w == TOMA_MX8 else ((C, hidden), (hidden, C))
-    w1, w2 = c.arg("W1", W1, w, up, _WEIGHT), c.arg("W2", W2, w, down, _WEIGHT)
-    _check(lib().toma_ffn(_ref(desc), c.arg("X", X, x, n), c.arg("R", R, x, n), c.arg("gamma", gamma, x, (C,)), w1,
-                          c.codes("W1s", W1s, hidden, C), c.arg("b1", b1, x, (hidden,)), w2,
-                          c.codes("W2s", W2s, C, hidden), c.arg("b2", b2, x, (C,)), c.arg("Y", Y, x, n), *c.scratch(ws), c.stream()),
+    w1, w2 = arg("W1", W1, t, up, _WEIGHT), arg("W2", W2, t, down, _WEIGHT)
+    _check(lib().toma_ffn(_ref(desc), arg("X", X, e, n), arg("R", R, e, n), arg("gamma", gamma, e, (C,)), w1, codes("W1s", W1s, hidden, C),
+                          arg("b1", b1, e, (hidden,)), w2, codes("W2s", W2s, C, hidden), arg("b2", b2, e, (C,)), arg("Y", Y, e, n),
+                          *c.scratch(ws), c.stream()),
            "toma_ffn")
 
 

@@ -101,5 +101,5 @@ def test_transposed_tensors_of_the_packing_calls_are_refused():
 def test_any_layout_of_whole_rows_is_taken(shape):
     """Rows one after the other: leading dimensions, heads as a dimension, several rows in one (the norm of single heads), flat."""
     t = dev(*shape)
-    assert tb._Call().arg("X", t, tb.TOMA_BF16, (6, 64)) == t.data_ptr()
-    assert tb._Call().arg("X", None, tb.TOMA_BF16, (6, 64)) is None
+    assert tb._Call().arg("X", t, BF, (6, 64)) == t.data_ptr()
+    assert tb._Call().arg("X", None, BF, (6, 64)) is None
